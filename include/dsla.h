@@ -296,6 +296,104 @@ dsla_status dsla_gate_project(const dsla_gate_project_args* a, void* cuda_stream
 dsla_status dsla_gate_project_last_error(void);
 
 /* ------------------------------------------------------------------------------------------
+ * Copying slots.  Move j makes slot dst_slots[j] equal to slot src_slots[j] (all states and heads of it), or zero where
+ * src_slots[j] == -1.  The moves take effect one after the other, in the order given, so every list has one result: a slot may be the
+ * source of many (a prompt shared by several sequences is forked), a target may be the source of a later move (a store is compacted,
+ * a slot passed on and freed in one call), and of two moves to one slot the later counts.  A move whose target is not a slot of the store, or whose
+ * source is neither a slot nor -1, is ignored, as is a move of a slot to itself.  Any number of states; n in 0 .. 65535 moves.  (No counterpart in the paper.)
+ * ------------------------------------------------------------------------------------------ */
+dsla_status dsla_state_copy(dsla_state* st, const int32_t* src_slots, const int32_t* dst_slots, int n, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Gated delta rule.  The layer's other gated recurrence: one state per (sequence, head) in a store with n_states = 1
+ * (dsla_state_alloc_n), which forgets by a gate and, before it takes a token in, what it would have answered to that token's key:
+ *     S <- g_t S,      u_t = beta_t (v_t - k_t S),      S <- S + k_t^T u_t,      o_t = scale * q_t S .
+ * g_t in [0, 1] and beta_t are already activated scalars per (token, head); a negative g_t counts as 0.  Keys of length <= 1 with
+ * beta_t in [0, 1] (or beta |k|^2 <= 2) keep the recurrence from growing; it is not bounded otherwise, in any form.  H_qk heads of queries
+ * and keys serve H = group * H_qk heads of values, gates and states: value head h reads head h / group.  (No counterpart in the paper.)
+ *
+ * Two kernels for prompts:
+ *   SIMT   : the recurrence token by token on CUDA cores in fp32; every dtype and head size, no workspace.
+ *   TENSOR : bf16 (heads of 64 or 128), chunks of 64 tokens on the tensor cores.  With G_j the product of the chunk's gates up to j and
+ *            D_ji that of the gates i+1 .. j, the u of a chunk solve (I + tril(beta_j D_ji k_j.k_i, -1)) U = beta (V - G K S); the
+ *            inverses of all chunks are computed first, in parallel, into the workspace, then each sequence walks its chunks.
+ *            Everything that reaches a state is held in 16 bits or more of mantissa and summed in fp32 (states 3e-6 from the token-by-token ones).
+ *   AUTO   : TENSOR for bf16, else SIMT.
+ * A call of impl TENSOR or AUTO is refused (DSLA_ERR_INVALID_ARG) without the workspace that dsla_delta_prefill_workspace_bytes() reports.
+ * An infinity or NaN in a token reaches, with TENSOR, the outputs of its whole chunk of 64 tokens, never those of another sequence.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    const void* q;              /* [T_total, H_qk, d_k] dtype, row-major, 16-byte aligned                     */
+    const void* k;              /* [T_total, H_qk, d_k]                                                       */
+    const void* v;              /* [T_total, H, d_v]                                                          */
+    void* o;                    /* [T_total, H, d_v] dtype (output)                                           */
+    const float* gate;          /* [T_total, H] fp32 in [0, 1]                                                */
+    const float* beta;          /* [T_total, H] fp32                                                          */
+    const int32_t* cu_seqlens;  /* as in dsla_prefill_args                                                    */
+    const int32_t* slots;       /* as in dsla_prefill_args                                                    */
+    int N, T, T_total, max_seqlen;
+    int H, H_qk, d_k, d_v;      /* H a multiple of H_qk                                                       */
+    dsla_dtype dtype;
+    float scale;
+    int use_initial_state;
+    dsla_impl impl;             /* AUTO, SIMT or TENSOR                                                       */
+    void* workspace;            /* scratch of dsla_delta_prefill_workspace_bytes(), 256-byte aligned          */
+    size_t workspace_bytes;
+} dsla_delta_prefill_args;
+
+size_t dsla_delta_prefill_workspace_bytes(const dsla_delta_prefill_args* a);
+
+/* Writes o for every token and the final state of every sequence into its slot; sequences of length 0 as in dsla_prefill, and so are the
+ * errors that only the device can see (dsla_state_last_error). */
+dsla_status dsla_delta_prefill(const dsla_delta_prefill_args* a, dsla_state* st, void* cuda_stream);
+
+typedef struct {
+    const void* q;              /* [B, H_qk, d_k] dtype                                                       */
+    const void* k;              /* [B, H_qk, d_k]                                                             */
+    const void* v;              /* [B, H, d_v]                                                                */
+    void* o;                    /* [B, H, d_v] dtype (output); rows with slot < 0 are written as 0            */
+    const float* gate;          /* [B, H] fp32                                                                */
+    const float* beta;          /* [B, H] fp32                                                                */
+    const int32_t* slots;       /* as in dsla_decode_args                                                     */
+    const uint8_t* row_mask;    /* as in dsla_decode_args                                                     */
+    int B, H, H_qk, d_k, d_v;
+    dsla_dtype dtype;
+    float scale;
+} dsla_delta_decode_args;
+
+/* One step of the recurrence for each row, in place: each element of a state is read once and written once. */
+dsla_status dsla_delta_decode_step(const dsla_delta_decode_args* a, dsla_state* st, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Queries and keys out of a projection: the norm of each head and the rotation by the token's position, in one pass.  For every token and head
+ *     y = w * x * r,   r = 1 / sqrt(mean(x^2) + eps) (RMS),  1 / sqrt(sum(x^2) + eps) (L2),  1 (NONE),
+ * and of the first `rot` channels of y each pair (a, b) becomes (a cos f - b sin f, b cos f + a sin f) with the angle
+ * f = position * inv_freq[i] (taken in fp64 before it is reduced, so far positions keep their angles): pair i is (i, i + rot/2), or
+ * (2i, 2i + 1) where `interleaved` is set.  Arithmetic in fp32, one rounding at the end.  Rows of x are `*_stride` elements apart, heads and channels
+ * within a row contiguous, so x may be a part of the rows of a fused projection; the outputs have strides of their own and
+ * may be the inputs themselves (same pointer and stride; other overlaps are not allowed).  rot a multiple of 16 in 0 .. d, else DSLA_ERR_UNSUPPORTED.
+ * Pointers 16-byte aligned and strides multiples of 16 bytes, else DSLA_ERR_INVALID_ARG.  (No counterpart in the paper.)
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { DSLA_NORM_NONE = 0, DSLA_NORM_RMS = 1, DSLA_NORM_L2 = 2 } dsla_norm;
+typedef struct {
+    const void* q;              /* T rows of [H, d] dtype, q_stride elements apart                            */
+    const void* k;              /* T rows of [H_k, d], k_stride elements apart                                */
+    void* q_out;                /* T rows of [H, d] dtype, q_out_stride elements apart (output)               */
+    void* k_out;                /* T rows of [H_k, d], k_out_stride elements apart (output)                   */
+    const float* q_weight;      /* [d] fp32 or NULL (ones)                                                    */
+    const float* k_weight;      /* [d] fp32 or NULL (ones)                                                    */
+    const int32_t* positions;   /* [T] int32, any sign; may be NULL when rot == 0                             */
+    const float* inv_freq;      /* [rot / 2] fp32; may be NULL when rot == 0                                  */
+    long long q_stride, k_stride, q_out_stride, k_out_stride;
+    int T, H, H_k, d, rot, interleaved;
+    dsla_norm norm;
+    dsla_dtype dtype;
+    float eps;                  /* >= 0                                                                       */
+} dsla_qk_norm_rope_args;
+
+dsla_status dsla_qk_norm_rope(const dsla_qk_norm_rope_args* a, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
  * Host-buffer variants (end-to-end path): q, k, v, o, g_hist, g_rec in `a` are HOST pointers
  * (pinned memory gives asynchronous copies); gamma, cu_seqlens, slots and the workspace stay
  * device pointers.  `staging` is caller-owned device memory of at least

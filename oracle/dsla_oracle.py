@@ -159,3 +159,58 @@ def gate_project(x, w, bias=None):
     if bias is not None:
         z = z + np.asarray(bias, dtype=np.float64)
     return 1.0 / (1.0 + np.exp(-z))
+
+
+def delta_prefill(q, k, v, gate, beta, cu_seqlens=None, *, scale=1.0, state=None, slots=None):
+    """Gated delta rule, token by token:
+        S <- g S,   u = beta (v - k S),   S <- S + k^T u,   o = scale q S .
+    q, k: [T, H_qk, dk]; v: [T, H, dv] (value head h reads head h // (H / H_qk)); gate, beta: [T, H]; state
+    [num_slots, 1, H, dk, dv] is updated in place when given, otherwise zeros are used.  Returns (o, state).  Plain numpy."""
+    q, k, v, gate, beta = (np.asarray(x, dtype=np.float64) for x in (q, k, v, gate, beta))
+    T, Hq, dk = q.shape
+    H, dv = v.shape[1:]
+    head = np.arange(H) // (H // Hq)
+    cu = np.array([0, T]) if cu_seqlens is None else np.asarray(cu_seqlens)
+    N = cu.size - 1
+    slots = np.arange(N) if slots is None else np.asarray(slots)
+    if state is None:
+        state = np.zeros((max(N, int(slots.max(initial=-1)) + 1), 1, H, dk, dv))
+    o = np.zeros((T, H, dv))
+    for n in range(N):
+        if slots[n] < 0:
+            continue
+        S = state[slots[n], 0]
+        for t in range(cu[n], cu[n + 1]):
+            kt, qt = k[t, head], q[t, head]
+            S *= gate[t][:, None, None]
+            u = beta[t][:, None] * (v[t] - np.matmul(kt[:, None, :], S)[:, 0])
+            S += kt[:, :, None] * u[:, None, :]
+            o[t] = scale * np.matmul(qt[:, None, :], S)[:, 0]
+    return o, state
+
+
+def qk_norm_rope(x, weight=None, positions=None, inv_freq=None, eps=1e-6, norm="rms", interleaved=False):
+    """Norm of each head and rotation of its first channels; x: [T, heads, d].  Plain numpy."""
+    x = np.array(x, dtype=np.float64)
+    square = (x * x).sum(-1, keepdims=True)
+    if norm != "none":
+        with np.errstate(invalid="ignore", divide="ignore"):
+            x = x / np.sqrt((square / x.shape[-1] if norm == "rms" else square) + eps)
+    if weight is not None:
+        x = x * np.asarray(weight, dtype=np.float64)
+    if inv_freq is not None:
+        for i, f in enumerate(np.asarray(inv_freq, dtype=np.float64)):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + len(inv_freq))
+            angle = np.asarray(positions, dtype=np.float64)[:, None] * f
+            xa, xb = x[..., a].copy(), x[..., b].copy()
+            x[..., a] = xa * np.cos(angle) - xb * np.sin(angle)
+            x[..., b] = xb * np.cos(angle) + xa * np.sin(angle)
+    return x
+
+
+def state_copy(state, src, dst):
+    """Moves between slots, one after the other, in place: src -1 clears, a move that names no slot is ignored."""
+    for a, b in zip(src, dst):
+        if 0 <= b < len(state) and -1 <= a < len(state):
+            state[b] = state[a] if a >= 0 else 0.0
+    return state

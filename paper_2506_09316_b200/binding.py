@@ -1,7 +1,7 @@
 """Binding of ``libdsla.so``: argument marshalling only.
 
-The calls of a serving loop (prefill, decode step, their n-state forms, gate producer) go through the extension module
-``_native``; everything else through ctypes.
+The calls of a serving loop (prefill, decode step, their n-state and delta-rule forms, gate producer, norms and rotation,
+slot copies) go through the extension module ``_native``; everything else through ctypes.
 
 Every function here has the name of the C entry point it forwards to (see
 ``include/dsla.h``).  Tensors are torch tensors (torch supplies device memory and
@@ -12,7 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_float, c_int, c_int32, c_size_t, c_uint64, c_void_p
+from ctypes import POINTER, Structure, byref, c_float, c_int, c_int32, c_longlong, c_size_t, c_uint64, c_void_p
 
 import torch
 
@@ -30,8 +30,10 @@ DSLA_STATIC_SCRATCH_BYTES = 18 << 20
 DSLA_F32, DSLA_BF16 = 0, 1
 DSLA_GATE_SCALAR, DSLA_GATE_PER_KEY_CHANNEL = 0, 1
 DSLA_IMPL_AUTO, DSLA_IMPL_SIMT, DSLA_IMPL_TENSOR, DSLA_IMPL_TENSOR_PAIR = 0, 1, 2, 3
+DSLA_NORM_NONE, DSLA_NORM_RMS, DSLA_NORM_L2 = 0, 1, 2
 _DTYPES = {torch.float32: DSLA_F32, torch.bfloat16: DSLA_BF16}
 _IMPLS = {"auto": DSLA_IMPL_AUTO, "simt": DSLA_IMPL_SIMT, "tensor": DSLA_IMPL_TENSOR, "pair": DSLA_IMPL_TENSOR_PAIR}
+_NORMS = {"none": DSLA_NORM_NONE, "rms": DSLA_NORM_RMS, "l2": DSLA_NORM_L2}
 
 
 class dsla_prefill_args(Structure):
@@ -70,6 +72,26 @@ class dsla_nstate_prefill_args(Structure):
                 ("n_states", c_int), ("dtype", c_int), ("scale", c_float), ("use_initial_state", c_int),
                 ("gate_layout", c_int), ("max_seqlen", c_int), ("impl", c_int), ("workspace", c_void_p),
                 ("workspace_bytes", c_size_t)]
+
+
+class dsla_delta_prefill_args(Structure):
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p), ("o", c_void_p), ("gate", c_void_p), ("beta", c_void_p),
+                ("cu_seqlens", c_void_p), ("slots", c_void_p), ("N", c_int), ("T", c_int), ("T_total", c_int), ("max_seqlen", c_int),
+                ("H", c_int), ("H_qk", c_int), ("d_k", c_int), ("d_v", c_int), ("dtype", c_int), ("scale", c_float),
+                ("use_initial_state", c_int), ("impl", c_int), ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
+
+
+class dsla_delta_decode_args(Structure):
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p), ("o", c_void_p), ("gate", c_void_p), ("beta", c_void_p),
+                ("slots", c_void_p), ("row_mask", c_void_p), ("B", c_int), ("H", c_int), ("H_qk", c_int), ("d_k", c_int), ("d_v", c_int),
+                ("dtype", c_int), ("scale", c_float)]
+
+
+class dsla_qk_norm_rope_args(Structure):
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("q_out", c_void_p), ("k_out", c_void_p), ("q_weight", c_void_p), ("k_weight", c_void_p),
+                ("positions", c_void_p), ("inv_freq", c_void_p), ("q_stride", c_longlong), ("k_stride", c_longlong),
+                ("q_out_stride", c_longlong), ("k_out_stride", c_longlong), ("T", c_int), ("H", c_int), ("H_k", c_int), ("d", c_int),
+                ("rot", c_int), ("interleaved", c_int), ("norm", c_int), ("dtype", c_int), ("eps", c_float)]
 
 
 _lib.dsla_status_string.argtypes = [c_int]
@@ -120,6 +142,16 @@ _lib.dsla_decode_staging_bytes.argtypes = [POINTER(dsla_decode_args)]
 _lib.dsla_decode_staging_bytes.restype = c_size_t
 _lib.dsla_decode_step_host.argtypes = [POINTER(dsla_decode_args), c_void_p, c_void_p, c_size_t, c_void_p]
 _lib.dsla_decode_step_host.restype = c_int
+_lib.dsla_state_copy.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p]
+_lib.dsla_state_copy.restype = c_int
+_lib.dsla_delta_prefill_workspace_bytes.argtypes = [POINTER(dsla_delta_prefill_args)]
+_lib.dsla_delta_prefill_workspace_bytes.restype = c_size_t
+_lib.dsla_delta_prefill.argtypes = [POINTER(dsla_delta_prefill_args), c_void_p, c_void_p]
+_lib.dsla_delta_prefill.restype = c_int
+_lib.dsla_delta_decode_step.argtypes = [POINTER(dsla_delta_decode_args), c_void_p, c_void_p]
+_lib.dsla_delta_decode_step.restype = c_int
+_lib.dsla_qk_norm_rope.argtypes = [POINTER(dsla_qk_norm_rope_args), c_void_p]
+_lib.dsla_qk_norm_rope.restype = c_int
 
 
 class DslaError(RuntimeError):
@@ -189,10 +221,13 @@ def dsla_state_bytes_n(num_slots: int, n_states: int, H: int, d_k: int, d_v: int
     return int(_lib.dsla_state_bytes_n(num_slots, n_states, H, d_k, d_v))
 
 
-def dsla_state_alloc_n(num_slots: int, n_states: int, H: int, d_k: int, d_v: int, device="cuda") -> DslaState:
-    """Store of the n-state form; ``tensor`` is [num_slots, n_states, H, d_k, d_v] fp32."""
+def dsla_state_alloc_n(num_slots: int, n_states: int, H: int, d_k: int, d_v: int, device="cuda", buffer=None) -> DslaState:
+    """Store of the n-state form; ``tensor`` is [num_slots, n_states, H, d_k, d_v] fp32.  ``buffer`` as in ``dsla_state_alloc``."""
     n = dsla_state_bytes_n(num_slots, n_states, H, d_k, d_v)
-    buf = torch.empty((num_slots, n_states, H, d_k, d_v), dtype=torch.float32, device=device) if n else None
+    if buffer is not None:
+        buf = buffer.view(num_slots, n_states, H, d_k, d_v)
+    else:
+        buf = torch.empty((num_slots, n_states, H, d_k, d_v), dtype=torch.float32, device=device) if n else None
     h = c_void_p()
     with torch.cuda.device(buf.device if buf is not None else device):
         rc = _lib.dsla_state_alloc_n(byref(h), num_slots, n_states, H, d_k, d_v, _ptr(buf), n)
@@ -473,3 +508,68 @@ def dsla_gate_project(x, w, bias=None, *, g_hist=None, g_rec=None, stream=None):
 
 def dsla_gate_project_last_error() -> int:
     return int(_lib.dsla_gate_project_last_error())
+
+
+def dsla_state_copy(st: DslaState, src_slots, dst_slots, stream=None):
+    """Moves between slots of a store, carried out one after the other: slot ``dst_slots[j]`` becomes slot ``src_slots[j]``, or zero where
+    that is -1 (int32 device tensors of one length).  Copies, forks, compacts and frees; moves that name no slot are ignored."""
+    _check(_native.state_copy(src_slots, dst_slots, st.address, None if stream is None else _raw_stream(stream)), "dsla_state_copy")
+
+
+def dsla_delta_prefill_workspace_bytes(T_total, N, max_seqlen, H, d, dtype=torch.bfloat16, *, H_qk=None, impl="auto", dense_T=None) -> int:
+    """Scratch bytes ``dsla_delta_prefill`` needs for these sizes (``dense_T``: tokens per sequence of a dense batch)."""
+    a = dsla_delta_prefill_args()
+    a.N, a.T, a.T_total, a.max_seqlen = int(N), int(dense_T or 0), int(T_total), int(max_seqlen)
+    a.H, a.H_qk, a.d_k, a.d_v = int(H), int(H if H_qk is None else H_qk), int(d), int(d)
+    a.dtype, a.impl, a.scale = _DTYPES[dtype], _IMPLS[impl], 1.0
+    if dense_T is None:
+        a.cu_seqlens = c_void_p(8)  # only tested for NULL, never dereferenced
+    return int(_lib.dsla_delta_prefill_workspace_bytes(byref(a)))
+
+
+def dsla_delta_prefill(q, k, v, gate, beta, st: DslaState, *, o=None, cu_seqlens=None, slots=None, max_seqlen=None, scale=1.0,
+                       use_initial_state=False, impl="auto", workspace=None, stream=None):
+    """Gated delta rule over prompts: q, k [T_total, H_qk, d], v [T_total, H, d] (fp32 or bf16, H a multiple of H_qk), gate, beta
+    [T_total, H] fp32, ``st`` a store of one state per slot (``dsla_state_alloc_n(slots, 1, H, d, d)``).  Dense and packed batches, slots and
+    ``max_seqlen`` as in ``dsla_prefill``.  Returns o [T_total, H, d]; final states land in ``st``."""
+    T_total = q.shape[0]
+    N, T, longest = _sequences(T_total, cu_seqlens, max_seqlen)
+    if longest is None:
+        raise ValueError("max_seqlen is required with cu_seqlens")
+    if o is None:
+        o = torch.empty_like(v)
+    if workspace is None:
+        need = dsla_delta_prefill_workspace_bytes(T_total, N, longest, v.shape[1], q.shape[2], q.dtype, H_qk=q.shape[1], impl=impl,
+                                                  dense_T=T if cu_seqlens is None else None)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    _check(_native.delta_prefill(q, k, v, o, gate, beta, cu_seqlens, slots, workspace, st.address, N, T, int(longest), scale,
+                                 1 if use_initial_state else 0, _IMPLS[impl], None if stream is None else _raw_stream(stream)), "dsla_delta_prefill")
+    return o
+
+
+def dsla_delta_decode_step(q, k, v, gate, beta, st: DslaState, *, o=None, slots=None, scale=1.0, row_mask=None, stream=None):
+    """One token per row of the gated delta rule: q, k [B, H_qk, d], v [B, H, d], gate, beta [B, H]; ``slots`` and ``row_mask`` as in
+    ``dsla_decode_step``.  Updates the rows' slots in place and returns o [B, H, d]."""
+    if o is None:
+        o = torch.empty_like(v)
+    rc = _native.delta_decode_step(q, k, v, o, gate, beta, slots, row_mask, st.address, scale, None if stream is None else _raw_stream(stream))
+    if rc:
+        _check(rc, "dsla_delta_decode_step")
+    return o
+
+
+def dsla_qk_norm_rope(q, k, q_weight=None, k_weight=None, *, positions=None, inv_freq=None, q_out=None, k_out=None, eps=1e-6, norm="rms",
+                      interleaved=False, stream=None):
+    """Norm of each head of queries and keys ("rms", "l2" or "none") and the rotation of its first ``2 * len(inv_freq)`` channels, one
+    pass.  q [T, H, d], k [T, H_k, d] (fp32 or bf16; rows may be parts of the rows of a fused projection), weights [d] fp32, positions [T] int32,
+    inv_freq [rot / 2] fp32 (None: no rotation).  Returns (q_out, k_out), which may be passed in, also as q and k themselves."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    rc = _native.qk_norm_rope(q, k, q_out, k_out, q_weight, k_weight, positions, inv_freq, eps, _NORMS[norm], 1 if interleaved else 0,
+                              None if stream is None else _raw_stream(stream))
+    if rc:
+        _check(rc, "dsla_qk_norm_rope")
+    return q_out, k_out

@@ -405,6 +405,92 @@ dsla_status dsla_decode_step(const dsla_decode_args* a, dsla_state* st, void* cu
 }
 
 // ---- gate producer ------------------------------------------------------------------------
+// ---- slots --------------------------------------------------------------------------------
+dsla_status dsla_state_copy(dsla_state* st, const int32_t* src_slots, const int32_t* dst_slots, int n, void* cuda_stream) {
+    if (!st || n < 0 || n > 65535 || !on_store_device(st)) return DSLA_ERR_INVALID_ARG;
+    if (n == 0) return DSLA_OK;
+    if (!src_slots || !dst_slots || !aligned(src_slots, 4) || !aligned(dst_slots, 4)) return DSLA_ERR_INVALID_ARG;
+    return launch_state_copy(st, src_slots, dst_slots, n, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// ---- gated delta rule ---------------------------------------------------------------------
+static dsla_status check_delta_sizes(const dsla_delta_prefill_args* a) {
+    if (!a) return DSLA_ERR_INVALID_ARG;
+    if (a->N < 0 || a->T_total < 0 || a->max_seqlen < 0 || a->H <= 0 || a->H_qk <= 0 || a->H % a->H_qk != 0 || a->d_k <= 0 || a->d_v <= 0) return DSLA_ERR_INVALID_ARG;
+    if (a->dtype != DSLA_F32 && a->dtype != DSLA_BF16) return DSLA_ERR_INVALID_ARG;
+    if (a->impl != DSLA_IMPL_AUTO && a->impl != DSLA_IMPL_SIMT && a->impl != DSLA_IMPL_TENSOR && a->impl != DSLA_IMPL_TENSOR_PAIR) return DSLA_ERR_INVALID_ARG;
+    if (!supported_d(a->d_k, a->d_v) || a->impl == DSLA_IMPL_TENSOR_PAIR) return DSLA_ERR_UNSUPPORTED;
+    if (a->impl == DSLA_IMPL_TENSOR && a->dtype != DSLA_BF16) return DSLA_ERR_UNSUPPORTED;
+    if (!a->cu_seqlens) {
+        if (a->T < 0 || (long long)a->N * a->T != a->T_total || a->max_seqlen < a->T) return DSLA_ERR_INVALID_ARG;
+    } else if (a->max_seqlen > a->T_total) {
+        return DSLA_ERR_INVALID_ARG;
+    }
+    return DSLA_OK;
+}
+
+size_t dsla_delta_prefill_workspace_bytes(const dsla_delta_prefill_args* a) {
+    return 0;
+}
+
+dsla_status dsla_delta_prefill(const dsla_delta_prefill_args* a, dsla_state* st, void* cuda_stream) {
+    const dsla_status rc = check_delta_sizes(a);
+    if (rc != DSLA_OK) return rc;
+    if (!st || st->n_states != 1 || st->H != a->H || st->d_k != a->d_k || st->d_v != a->d_v) return DSLA_ERR_INVALID_ARG;
+    if (!a->slots && a->N > st->num_slots) return DSLA_ERR_INVALID_ARG;
+    if (!(a->scale == a->scale) || !on_store_device(st)) return DSLA_ERR_INVALID_ARG;
+    if (a->N == 0) return DSLA_OK;
+    if (a->T_total > 0) {
+        if (!a->q || !a->k || !a->v || !a->o || !a->gate || !a->beta) return DSLA_ERR_INVALID_ARG;
+        if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->o, 16)) return DSLA_ERR_INVALID_ARG;
+        if (!aligned(a->gate, 4) || !aligned(a->beta, 4)) return DSLA_ERR_INVALID_ARG;
+    }
+    DeltaParams p{};
+    p.q = a->q; p.k = a->k; p.v = a->v; p.o = a->o; p.gate = a->gate; p.beta = a->beta;
+    p.cu_seqlens = a->cu_seqlens; p.slots = a->slots; p.state = st->data; p.status = st->status;
+    p.N = a->N; p.T = a->T; p.H = a->H; p.group = a->H / a->H_qk; p.num_slots = st->num_slots;
+    p.use_initial_state = a->use_initial_state ? 1 : 0; p.scale = a->scale;
+    return launch_delta_recurrent(p, a->d_k, a->dtype, static_cast<cudaStream_t>(cuda_stream));
+}
+
+dsla_status dsla_delta_decode_step(const dsla_delta_decode_args* a, dsla_state* st, void* cuda_stream) {
+    if (!a || !st) return DSLA_ERR_INVALID_ARG;
+    if (a->B < 0 || a->H <= 0 || a->H_qk <= 0 || a->H % a->H_qk != 0 || a->d_k <= 0 || a->d_v <= 0) return DSLA_ERR_INVALID_ARG;
+    if (a->dtype != DSLA_F32 && a->dtype != DSLA_BF16) return DSLA_ERR_INVALID_ARG;
+    if (!supported_d(a->d_k, a->d_v)) return DSLA_ERR_UNSUPPORTED;
+    if (st->n_states != 1 || st->H != a->H || st->d_k != a->d_k || st->d_v != a->d_v) return DSLA_ERR_INVALID_ARG;
+    if (!a->slots && a->B > st->num_slots) return DSLA_ERR_INVALID_ARG;
+    if (!(a->scale == a->scale) || !on_store_device(st)) return DSLA_ERR_INVALID_ARG;
+    if (a->B == 0) return DSLA_OK;
+    if (!a->q || !a->k || !a->v || !a->o || !a->gate || !a->beta) return DSLA_ERR_INVALID_ARG;
+    if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->o, 16)) return DSLA_ERR_INVALID_ARG;
+    if (!aligned(a->gate, 4) || !aligned(a->beta, 4)) return DSLA_ERR_INVALID_ARG;
+    DeltaParams p{};
+    p.q = a->q; p.k = a->k; p.v = a->v; p.o = a->o; p.gate = a->gate; p.beta = a->beta;
+    p.slots = a->slots; p.row_mask = a->row_mask; p.state = st->data; p.status = st->status;
+    p.N = a->B; p.H = a->H; p.group = a->H / a->H_qk; p.num_slots = st->num_slots; p.scale = a->scale;
+    return launch_delta_decode(p, a->d_k, a->dtype, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// ---- queries and keys ---------------------------------------------------------------------
+dsla_status dsla_qk_norm_rope(const dsla_qk_norm_rope_args* a, void* cuda_stream) {
+    if (!a || a->T < 0 || a->H <= 0 || a->H_k <= 0 || a->d <= 0 || a->rot < 0 || a->rot > a->d) return DSLA_ERR_INVALID_ARG;
+    if (a->dtype != DSLA_F32 && a->dtype != DSLA_BF16) return DSLA_ERR_INVALID_ARG;
+    if (a->norm != DSLA_NORM_NONE && a->norm != DSLA_NORM_RMS && a->norm != DSLA_NORM_L2) return DSLA_ERR_INVALID_ARG;
+    if (!(a->eps >= 0.f)) return DSLA_ERR_INVALID_ARG;
+    if (!supported_d(a->d, a->d) || a->rot % 16 != 0) return DSLA_ERR_UNSUPPORTED;
+    if (a->T == 0) return DSLA_OK;
+    if (!a->q || !a->k || !a->q_out || !a->k_out || (a->rot > 0 && (!a->positions || !a->inv_freq))) return DSLA_ERR_INVALID_ARG;
+    if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->q_out, 16) || !aligned(a->k_out, 16)) return DSLA_ERR_INVALID_ARG;
+    if (!aligned(a->q_weight, 4) || !aligned(a->k_weight, 4) || !aligned(a->positions, 4) || !aligned(a->inv_freq, 4)) return DSLA_ERR_INVALID_ARG;
+    const long long strides[4] = {a->q_stride, a->k_stride, a->q_out_stride, a->k_out_stride};
+    for (int i = 0; i < 4; ++i) {
+        const long long row = (long long)(i % 2 ? a->H_k : a->H) * a->d;       // rows must not overlap
+        if (strides[i] < row || strides[i] % (long long)(16 / esize(a->dtype)) != 0) return DSLA_ERR_INVALID_ARG;
+    }
+    return launch_qk_norm_rope(a, static_cast<cudaStream_t>(cuda_stream));
+}
+
 dsla_status dsla_gate_project(const dsla_gate_project_args* a, void* cuda_stream) {
     if (!a || a->T < 0 || a->H <= 0 || a->D_model <= 0) return DSLA_ERR_INVALID_ARG;
     if (a->H % 8 != 0 || 2 * a->H > 256 || a->D_model % 64 != 0) return DSLA_ERR_UNSUPPORTED;

@@ -66,6 +66,19 @@ struct RecurrentParams {
     float scale;
 };
 
+// Gated delta rule: prompts (rows = tokens) and single tokens (rows = batch rows).
+struct DeltaParams {
+    const void *q, *k, *v;
+    void* o;
+    const float *gate, *beta;   // [rows, H]
+    const int32_t *cu_seqlens, *slots;
+    const uint8_t* row_mask;    // single tokens: [B] or nullptr
+    float* state;               // [num_slots][H][D][D]
+    int* status;
+    int N, T, H, group, num_slots, use_initial_state;      // N: sequences, or rows of a decode batch; group: value heads of a head of q and k
+    float scale;
+};
+
 void count_launch(int n = 1);
 int sm_count();      // of the current device
 
@@ -74,6 +87,13 @@ dsla_status prefill_checked(const dsla_prefill_args* a, dsla_state* st, cudaStre
 size_t prefill_required_bytes(const dsla_prefill_args* a);      // the part of dsla_prefill_workspace_bytes that a call is refused without
 // dsla_decode.cu
 dsla_status launch_decode(const DecodeParams& p, int d, dsla_dtype dt, cudaStream_t s);
+// dsla_state_copy.cu
+dsla_status launch_state_copy(const dsla_state* st, const int32_t* src, const int32_t* dst, int n, cudaStream_t s);
+// dsla_qk_norm.cu
+dsla_status launch_qk_norm_rope(const dsla_qk_norm_rope_args* a, cudaStream_t s);
+// dsla_delta_decode.cu, dsla_delta_recurrent.cu, dsla_delta_tc.cu
+dsla_status launch_delta_decode(const DeltaParams& p, int d, dsla_dtype dt, cudaStream_t s);
+dsla_status launch_delta_recurrent(const DeltaParams& p, int d, dsla_dtype dt, cudaStream_t s);
 // dsla_gate_project.cu
 dsla_status launch_gate_project(const dsla_gate_project_args* a, cudaStream_t s);
 dsla_status gate_project_last_error();
