@@ -429,8 +429,10 @@ static dsla_status check_delta_sizes(const dsla_delta_prefill_args* a) {
     return DSLA_OK;
 }
 
+static bool delta_on_tensor_cores(const dsla_delta_prefill_args* a) { return a->dtype == DSLA_BF16 && a->impl != DSLA_IMPL_SIMT; }
+
 size_t dsla_delta_prefill_workspace_bytes(const dsla_delta_prefill_args* a) {
-    return 0;
+    return check_delta_sizes(a) == DSLA_OK && delta_on_tensor_cores(a) ? delta_tc_workspace_bytes(a) : 0;
 }
 
 dsla_status dsla_delta_prefill(const dsla_delta_prefill_args* a, dsla_state* st, void* cuda_stream) {
@@ -445,11 +447,14 @@ dsla_status dsla_delta_prefill(const dsla_delta_prefill_args* a, dsla_state* st,
         if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->o, 16)) return DSLA_ERR_INVALID_ARG;
         if (!aligned(a->gate, 4) || !aligned(a->beta, 4)) return DSLA_ERR_INVALID_ARG;
     }
+    const size_t need = dsla_delta_prefill_workspace_bytes(a);
+    if (need > 0 && (!a->workspace || a->workspace_bytes < need || !aligned(a->workspace, 256))) return DSLA_ERR_INVALID_ARG;
     DeltaParams p{};
     p.q = a->q; p.k = a->k; p.v = a->v; p.o = a->o; p.gate = a->gate; p.beta = a->beta;
     p.cu_seqlens = a->cu_seqlens; p.slots = a->slots; p.state = st->data; p.status = st->status;
     p.N = a->N; p.T = a->T; p.H = a->H; p.group = a->H / a->H_qk; p.num_slots = st->num_slots;
     p.use_initial_state = a->use_initial_state ? 1 : 0; p.scale = a->scale;
+    if (delta_on_tensor_cores(a)) return launch_delta_tc(p, a, static_cast<cudaStream_t>(cuda_stream));
     return launch_delta_recurrent(p, a->d_k, a->dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 
