@@ -1,14 +1,15 @@
 // Gated delta rule over prompts on the tensor cores (bf16, heads of 64 or 128), in chunks of 64 tokens:
 //     S <- g S,   u = beta (v - k S),   S <- S + k^T u,   o = scale q S .
 // With L_j the sum of log2 g up to token j of the chunk, G_j = 2^L_j, D_ji = 2^(L_j - L_i) and
-//     A = tril(beta_j D_ji k_j.k_i, -1),   T = (I + A)^-1 diag(beta),   P = scale tril(D_ji q_j.k_i),   R = V - G K S ,
-// a chunk is       U = T R,       O = scale G Q S + (P T) R,       S <- G_63 S + K^T diag(2^(L_63 - L)) U .
-// T and P T need no state: a first kernel computes them for all chunks at once (one CTA per chunk and head) into the workspace, a second one walks the
-// chunks of each sequence, three dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v).
+//     A = tril(beta_j D_ji k_j.k_i, -1),   T = (I + A)^-1 diag(beta),   P = scale tril(D_ji q_j.k_i),   Y = K^T diag(2^(L_63 - L)) T
+// a chunk is
+//     R = V - G K S,       O = scale G Q S + (P T) R,       S <- G_63 S + Y R .
+// Y and P T need no state: a first kernel computes them for all chunks at once (one CTA per chunk and head) into the workspace, a second one walks the
+// chunks of each sequence, two dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v).
 //
-// Precision.  K, Q, V are bf16 as they come.  What reaches a state is held in two bf16 terms (16 bits of mantissa: S as the operand of K S, R, T
-// below its diagonal, U, both factors of P T) with fp32 sums; T's diagonal, beta, is applied in fp32, where most of U comes from when keys differ.  The state itself stays in fp32
-// registers and each chunk adds one tensor-core sum to it, with rounding.  What reaches only the bf16 output (S as the operand of Q S, P T as a factor) has one term.
+// Precision.  K, Q, V are bf16 as they come.  What reaches a state is held in two bf16 terms (16 bits of mantissa: S as the operand of K S, R, Y) or three (what
+// Y is made of), with fp32 sums; (I + A)^-1 is fp32.  The state itself stays in fp32 registers and each chunk adds one tensor-core sum to
+// it, with rounding.  P T, which reaches only the bf16 output, has one term.
 #include <cuda.h>
 
 #include "dsla_internal.cuh"
@@ -25,9 +26,12 @@ namespace {
 
 constexpr int DC = 64;                          // tokens per chunk
 constexpr int TILE = DC * 128;                  // bytes of 64 rows of 64 bf16
-// A chunk in the workspace: T (high terms), P T, T (low terms), each [64][64] bf16 as the MMA reads it (128-byte swizzle), then scale G, G, beta and
-// 2^(L_63 - L), each [64] fp32.  T_hi above P T are the 128 rows of one operand.
-constexpr int CHUNK_TILES = 3 * TILE, CHUNK_BYTES = CHUNK_TILES + 4 * DC * 4;
+// A chunk in the workspace: Y's high terms and its low terms, each [d][64] bf16, and P T [64][64] bf16, as the MMAs read them (128-byte swizzle), then scale G
+// and G, each [64] fp32.
+template <int D>
+struct Chunk {
+    static constexpr int Y = D * 128, PT = 2 * Y, META = PT + TILE, BYTES = META + 2 * DC * 4;
+};
 
 struct DeltaTcParams {
     DeltaParams p;
@@ -40,6 +44,9 @@ struct DeltaTcParams {
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
                  : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
@@ -59,6 +66,34 @@ __device__ __forceinline__ void find_sequence(const DeltaTcParams& tp, int n, in
     }
 }
 
+// Pairs of fp32: one instruction for two.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair(uint32_t x, uint32_t y) { return pair(__uint_as_float(x), __uint_as_float(y)); }
+__device__ __forceinline__ float2 unpair(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
+}
+
 // x in two bf16 terms, high and low.
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
     hi = pack_bf16(x, y);
@@ -66,38 +101,91 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
     lo = pack_bf16(x - h.x, y - h.y);
 }
 
-// 32 fp32 values in two bf16 terms into row r of an operand whose rows hold [32 high | 32 low].
-__device__ __forceinline__ void put_split(uint8_t* tile, int r, const float (&x)[32]) {
-    uint8_t* row = tile + r * 128;
+#define WAIT(bar, parity) mbar_wait(bar, parity, abortp, p.status)
+
+// ------------------------------------------------------------------------------------------------ Y and P T of every chunk
+// Eight warps, two to a lane quadrant (columns 0..31 and 32..63).  [K; Q] K^T is one MMA of 128 rows; quadrants 0, 1 turn its upper half into A, 2, 3 its lower half
+// into P.  (I + A)^-1 in fp32: the four diagonal blocks of 16 by substitution, one column per thread, then twice
+//     [a 0; b c]^-1 = [a^-1 0; -c^-1 b a^-1 c^-1]
+// for pairs of blocks of 16 and of 32, columns eight to a warp, as TF32 products of two terms each (22 bits).  Then Y and P T are MMAs.  (A substitution over all 64
+// rows by 64 threads, 2016 steps of the chain each, and T written two bytes at a time took 110 us for 4096 tokens of 32 heads.)
+constexpr int PREP_THREADS = 256;
+constexpr int XP = 68;                                          // pitch of A and of the inverse in shared memory, floats
+constexpr int PREP_A = 0, PREP_X = DC * XP * 4, PREP_SCRATCH = 2 * PREP_X;      // behind K and Q; scratch: [32][8] floats of four warps
+constexpr int PREP_T = 0, PREP_W = 2 * TILE;                    // the same room later: T in two terms, diag(2^(L_63 - L)) T in three
+constexpr int PREP_WORK = 5 * TILE;
+static_assert(PREP_SCRATCH + 4 * 32 * 8 * 4 <= PREP_WORK, "A, the inverse and the scratch fit where T will be");
+
+template <int D>
+struct Prep {
+    // P's high terms take the place of Q's first tile, the low ones that of its second (d = 64 has none: one more)
+    static constexpr int KQ = 2 * TILE * (D / 64), P_LO = D == 128 ? 3 * TILE : KQ + PREP_WORK;
+    static constexpr int META = KQ + PREP_WORK + (D == 128 ? 0 : TILE), SMEM = META + 2 * DC * 4 + 1024;
+};
+
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void tf32_terms(float x, uint32_t& hi, uint32_t& lo) {
+    hi = __float_as_uint(x) & 0xffffe000u;
+    lo = __float_as_uint(x - __uint_as_float(hi));
+}
+// c[m tile] += M[16 MT x 8 KT] B[8 KT x 8], both in shared memory (row pitches pa, pb), as products of two TF32 terms.
+template <int MT, int KT>
+__device__ __forceinline__ void product(float (&c)[MT][4], const float* M, int pa, const float* B, int pb, int lane) {
+    const int r = lane >> 2, q = lane & 3;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t h[4], l[4];
+    for (int k = 0; k < KT; ++k) {
+        uint32_t bh[2], bl[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], h[e], l[e]);
-        *reinterpret_cast<uint4*>(row + ((i ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4*>(row + (((i + 4) ^ (r & 7)) << 4)) = make_uint4(l[0], l[1], l[2], l[3]);
+        for (int i = 0; i < 2; ++i) tf32_terms(B[(8 * k + q + 4 * i) * pb + r], bh[i], bl[i]);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            uint32_t ah[4], al[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tf32_terms(M[(16 * m + r + 8 * (i & 1)) * pa + 8 * k + q + 4 * (i >> 1)], ah[i], al[i]);
+            mma_tf32(c[m], al, bh);
+            mma_tf32(c[m], ah, bl);
+            mma_tf32(c[m], ah, bh);
+        }
+    }
+}
+// Columns n0 .. n0 + 7 of the lower left block of the inverse: rows r0 .., columns c0 .., blocks of 16 MT.
+template <int MT>
+__device__ __forceinline__ void lower_left(const float* A, float* X, float* scratch, int r0, int c0, int n0, int lane) {
+    float c[MT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0.f;
+    product<MT, 2 * MT>(c, A + r0 * XP + c0, XP, X + c0 * XP + c0 + n0, XP, lane);
+    const int r = lane >> 2, q = lane & 3;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        *reinterpret_cast<float2*>(scratch + (16 * m + r) * 8 + 2 * q) = make_float2(-c[m][0], -c[m][1]);
+        *reinterpret_cast<float2*>(scratch + (16 * m + r + 8) * 8 + 2 * q) = make_float2(-c[m][2], -c[m][3]);
+        c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0.f;
+    }
+    __syncwarp();
+    product<MT, 2 * MT>(c, X + r0 * XP + r0, XP, scratch, 8, lane);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        *reinterpret_cast<float2*>(X + (r0 + 16 * m + r) * XP + c0 + n0 + 2 * q) = make_float2(c[m][0], c[m][1]);
+        *reinterpret_cast<float2*>(X + (r0 + 16 * m + r + 8) * XP + c0 + n0 + 2 * q) = make_float2(c[m][2], c[m][3]);
     }
 }
 
-#define WAIT(bar, parity) mbar_wait(bar, parity, abortp, p.status)
-
-// ------------------------------------------------------------------------------------------------ T and P T of every chunk
-// Four warps.  [K; Q] K^T is one MMA of 128 rows; warps 0, 1 turn its upper half into A, warps 2, 3 its lower half into P.  Then 64 threads solve (I + A) T =
-// diag(beta), one column each, in fp32: x_i is final at step i and leaves A_ji x_i in every later x_j, so a step's products are independent of each
-// other.  P T is a second MMA.  The tiles of K and Q make room for what is made of them.
-constexpr int PREP_THREADS = 128;
-constexpr int PREP_A = 0;                                   // A transposed, [column][row] fp32; then P's low terms in the second tile
-constexpr int PREP_T_HI = 2 * TILE, PREP_P = 3 * TILE, PREP_T_LO = 4 * TILE, PREP_META = 5 * TILE;
-constexpr int PREP_SMEM = PREP_META + 4 * DC * 4 + 1024;    // K and Q: from 0 on, 2 tiles (d = 64) or 4
-
 template <int D>
-__global__ void __launch_bounds__(PREP_THREADS) delta_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const DeltaTcParams tp) {
+__global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const DeltaTcParams tp) {
+    using L = Prep<D>;
+    using Out = Chunk<D>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full, done;
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
-    __shared__ float lhi[DC], llo[DC], sbeta[DC];
+    __shared__ __align__(16) float lhi[DC], llo[DC], sbeta[DC], sw[DC], sleft[DC / 2];
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
+    uint8_t* work = sm + L::KQ;
     const DeltaParams& p = tp.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abortp = &abort_flag;
@@ -126,21 +214,15 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_chunk_kernel(const __grid_
         mbar_init(&done, 1);
         abort_flag = 0;
         fence_barrier_init();
-    }
-    if (warp == 1) { tmem_alloc(&tmem_base, 64); tmem_relinquish(); }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tb = tmem_base;
-    if (tid == 0) {
         const int hq = h / p.group;
-        mbar_arrive_expect_tx(&full, 2 * TILE * (D / 64));
+        mbar_arrive_expect_tx(&full, L::KQ);
         for (int half = 0; half < D / 64; ++half) {      // rows 0..63 K, 64..127 Q
             tma_load_4d(sm + half * 2 * TILE, &map_k, &full, 0, t0, half, hq);
             tma_load_4d(sm + half * 2 * TILE + TILE, &map_q, &full, 0, t0, half, hq);
         }
     }
-    if (warp == 1) {
+    if (warp == 1) { tmem_alloc(&tmem_base, 128); tmem_relinquish(); }
+    if (warp == 2) {
         // sums of logs in fp64, handed on as two floats: differences of neighbours stay exact however far the sum has run
         double run[2];
         float beta[2];
@@ -162,8 +244,8 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_chunk_kernel(const __grid_
         }
         run[0] += total - run[1];
         run[1] = total;
-        const double last = __shfl_sync(0xffffffffu, total, 31);
-        float* meta = reinterpret_cast<float*>(sm + PREP_META);
+        const double last = __shfl_sync(0xffffffffu, total, 31), middle = __shfl_sync(0xffffffffu, total, 15);
+        float* meta = reinterpret_cast<float*>(sm + L::META);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * lane + i;
@@ -171,12 +253,17 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_chunk_kernel(const __grid_
             lhi[j] = hi;
             llo[j] = (float)(run[i] - hi);
             sbeta[j] = beta[i];
+            sw[j] = ex2((float)(last - run[i]));
+            if (j < 32) sleft[j] = ex2((float)(middle - run[i]));
             meta[j] = G * p.scale;
             meta[DC + j] = G;
-            meta[2 * DC + j] = beta[i];
-            meta[3 * DC + j] = ex2((float)(last - run[i]));
         }
-    } else if (tid == 0) {
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tb = tmem_base;
+    if (tid == 0) {
         WAIT(&full, 0);
         tc_fence_after();
         const uint32_t kq = smem_u32(sm);
@@ -188,140 +275,257 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_chunk_kernel(const __grid_
         }
         tc_commit(&done);
     }
-    __syncthreads();
+    __syncwarp();
+    const int quad = warp & 3, part = warp >> 2, row = 32 * quad + lane, j = row & 63, upper = quad & 1;
+    const uint32_t row_addr = tb + ((uint32_t)(32 * quad) << 16) + 32 * part;
+    float* A = reinterpret_cast<float*>(work + PREP_A);
+    float* X = reinterpret_cast<float*>(work + PREP_X);
+    const bool is_p = quad >= 2;
     WAIT(&done, 0);
     tc_fence_after();
-    const int j = tid & 63;
-    const uint32_t row_addr = tb + ((uint32_t)(32 * warp) << 16);
-    const float hj = lhi[j], lj = llo[j], bj = sbeta[j];
-    float* at_ = reinterpret_cast<float*>(sm + PREP_A);
-    uint32_t pw[32], pl[32];      // warps 2, 3: row j of P, bf16 pairs, and their low terms
+    if (live < DC)      // rows of K behind the end meet zeros of T in Y: whatever they hold must be finite
+        for (int i = live * 8 + tid; i < DC * 8; i += PREP_THREADS)
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        uint32_t r[32];
-        tmem_ld32(row_addr + 32 * half, r);
-        tc_wait_ld();
+            for (int half = 0; half < D / 64; ++half) *reinterpret_cast<uint4*>(sm + half * 2 * TILE + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    if (upper >= part) {
+        float x[32];
+        {
+            uint32_t r[32];
+            tmem_ld32(row_addr, r);
+            tc_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            float x[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int s = 32 * half + i + e;
-                x[e] = __uint_as_float(r[i + e]) * ex2((hj - lhi[s]) + (lj - llo[s]));
-                if (warp < 2) at_[s * DC + j] = s < j && j < live ? bj * x[e] : 0.f;
-                else x[e] = s <= j && j < live ? p.scale * x[e] : 0.f;
-            }
-            split2(x[0], x[1], pw[16 * half + i / 2], pl[16 * half + i / 2]);
+            for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
         }
-    }
-    if (warp >= 2) {
+        const float f = j < live ? (is_p ? p.scale : sbeta[j]) : 0.f;
+        if (upper == part) {      // a diagonal block of 32
+            const float hj = lhi[j], lj = llo[j];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(sm + PREP_P + j * 128 + ((i ^ (j & 7)) << 4)) = make_uint4(pw[4 * i], pw[4 * i + 1], pw[4 * i + 2], pw[4 * i + 3]);
+            for (int i = 0; i < 32; i += 4) {
+                const float4 hs = *reinterpret_cast<const float4*>(lhi + 32 * part + i), ls = *reinterpret_cast<const float4*>(llo + 32 * part + i);
+                x[i] *= f * ex2((hj - hs.x) + (lj - ls.x));
+                x[i + 1] *= f * ex2((hj - hs.y) + (lj - ls.y));
+                x[i + 2] *= f * ex2((hj - hs.z) + (lj - ls.z));
+                x[i + 3] *= f * ex2((hj - hs.w) + (lj - ls.w));
+            }
+        } else {                  // left of it: through the sum up to token 31
+            const float fr = f * ex2((lhi[j] - lhi[31]) + (llo[j] - llo[31]));
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const float4 l = *reinterpret_cast<const float4*>(sleft + i);
+                x[i] *= fr * l.x; x[i + 1] *= fr * l.y; x[i + 2] *= fr * l.z; x[i + 3] *= fr * l.w;
+            }
+        }
+        const int last = j >= live ? -1 : is_p ? j : j - 1;      // columns up to this one
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = 32 * part + i <= last ? x[i] : 0.f;
+        if (!is_p) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(A + j * XP + 32 * part + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], hi[e], lo[e]);
+                const int at16 = j * 128 + (((4 * part + i) ^ (j & 7)) << 4);
+                *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+        }
+    } else if (is_p) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at16 = j * 128 + (((4 * part + i) ^ (j & 7)) << 4);
+            *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(0u, 0u, 0u, 0u);
+        }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp < 2) {
-        float x[DC];
+    if (warp < 2) {      // diagonal blocks of 16: thread = column
+        const int b0 = 16 * (tid >> 4), col = tid & 15;
+        float x[16];
 #pragma unroll
-        for (int i = 0; i < DC; ++i) x[i] = i == j ? bj : 0.f;
+        for (int i = 0; i < 16; ++i) {
+            float s[4] = {i == col ? 1.f : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < DC - 1; ++s) {
-            if (s < 32 && warp == 1) continue;      // columns 32.. begin at row 32
-            const float xs = x[s];
-#pragma unroll
-            for (int i = (s + 1) & ~3; i < DC; i += 4) {
-                const float4 a = *reinterpret_cast<const float4*>(at_ + s * DC + i);
-                if (i > s) x[i] = fmaf(-a.x, xs, x[i]);
-                if (i + 1 > s) x[i + 1] = fmaf(-a.y, xs, x[i + 1]);
-                if (i + 2 > s) x[i + 2] = fmaf(-a.z, xs, x[i + 2]);
-                if (i + 3 > s) x[i + 3] = fmaf(-a.w, xs, x[i + 3]);
+            for (int k = 0; k < i; k += 4) {
+                const float4 a = *reinterpret_cast<const float4*>(A + (b0 + i) * XP + b0 + k);
+                s[0] = fmaf(-a.x, x[k], s[0]);
+                if (k + 1 < i) s[1] = fmaf(-a.y, x[k + 1], s[1]);
+                if (k + 2 < i) s[2] = fmaf(-a.z, x[k + 2], s[2]);
+                if (k + 3 < i) s[3] = fmaf(-a.w, x[k + 3], s[3]);
             }
+            x[i] = (s[0] + s[1]) + (s[2] + s[3]);
+            X[(b0 + i) * XP + b0 + col] = x[i];
         }
+    } else if (warp < 4) {      // right of the diagonal blocks the products read zeros
+        const int i = tid - 64;
 #pragma unroll
-        for (int i = 0; i < DC; ++i) {
-            const float y = i > j ? x[i] : 0.f;      // below the diagonal
-            const __nv_bfloat16 hi = __float2bfloat16_rn(y);
-            const uint32_t off = sw128_offset(i, j);
-            *reinterpret_cast<__nv_bfloat16*>(sm + PREP_T_HI + off) = hi;
-            *reinterpret_cast<__nv_bfloat16*>(sm + PREP_T_LO + off) = __float2bfloat16_rn(y - __bfloat162float(hi));
-        }
+        for (int k = 0; k < 2; ++k)
+            *reinterpret_cast<float4*>(X + (32 * k + (i >> 2)) * XP + 32 * k + 16 + 4 * (i & 3)) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncthreads();
-    if (warp >= 2) {
+    float* scratch = reinterpret_cast<float*>(work + PREP_SCRATCH) + (warp & 3) * 256;
+    if (warp < 4) lower_left<1>(A, X, scratch, 32 * (warp >> 1) + 16, 32 * (warp >> 1), 8 * (warp & 1), lane);
+    __syncthreads();
+    if (warp < 4) lower_left<2>(A, X, scratch, 32, 0, 8 * warp, lane);
+    __syncthreads();
+    {
+        // T = inverse diag(beta) and its rows weighted, into tiles; thread = 16 columns of a row
+        const int s = tid >> 2, c0 = 16 * (tid & 3);
+        float x[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(sm + PREP_A + TILE + j * 128 + ((i ^ (j & 7)) << 4)) = make_uint4(pl[4 * i], pl[4 * i + 1], pl[4 * i + 2], pl[4 * i + 3]);
+        for (int i = 0; i < 16; i += 4) {
+            const float4 y = *reinterpret_cast<const float4*>(X + s * XP + c0 + i), b = *reinterpret_cast<const float4*>(sbeta + c0 + i);
+            x[i] = c0 + i <= s ? y.x * b.x : 0.f;
+            x[i + 1] = c0 + i + 1 <= s ? y.y * b.y : 0.f;
+            x[i + 2] = c0 + i + 2 <= s ? y.z * b.z : 0.f;
+            x[i + 3] = c0 + i + 3 <= s ? y.w * b.w : 0.f;
+        }
+        const float w = sw[s];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t t[2][4], y[3][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float u = x[8 * i + 2 * e], v = x[8 * i + 2 * e + 1];
+                split2(u, v, t[0][e], t[1][e]);
+                const float uw = u * w, vw = v * w;
+                y[0][e] = pack_bf16(uw, vw);
+                const float2 hi = unpack_bf16(y[0][e]);
+                split2(uw - hi.x, vw - hi.y, y[1][e], y[2][e]);
+            }
+            uint8_t* to = work + s * 128 + (((c0 / 8 + i) ^ (s & 7)) << 4);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(to + PREP_T + k * TILE) = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to + PREP_W + k * TILE) = make_uint4(y[k][0], y[k][1], y[k][2], y[k][3]);
+        }
     }
     fence_proxy_async_smem();
     __syncthreads();
     if (tid == 0) {
         tc_fence_after();
+        const uint32_t kt = smem_u32(sm), tt = smem_u32(work + PREP_T), wt = smem_u32(work + PREP_W);
+        // Y: d = 64 has 64 rows, the other half of the product is not read
+        constexpr uint32_t ID_Y = idesc_bf16(128, 64, 1, 1), ID_P = idesc_bf16(128, 64, 0, 1);
+#pragma unroll
+        for (int k = 2; k >= 0; --k)
+#pragma unroll
+            for (int kk = 0; kk < DC / 16; ++kk)
+                mma_ss(tb + 64, smem_desc_sw128(kt + kk * 2048, 2 * TILE, 1024), smem_desc_sw128(wt + k * TILE + kk * 2048, 16, 1024), ID_Y, k < 2 || kk ? 1u : 0u);
         // P T cancels where keys are alike (its rows are differences of P's), so both factors keep two terms.  Rows 64..127 of the operands are P; the
-        // products of the first 64 are not read.
-        const uint32_t p_hi = smem_u32(sm + PREP_T_HI), p_lo = smem_u32(sm + PREP_A), t_hi = smem_u32(sm + PREP_T_HI), t_lo = smem_u32(sm + PREP_T_LO);
-        constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
+        // products of the 64 rows before them are not read.
+        const uint32_t p_hi = smem_u32(sm), p_lo = smem_u32(sm + L::P_LO - TILE);
 #pragma unroll
-        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_lo + kk * 32, 16, 1024), smem_desc_sw128(t_hi + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
+        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_lo + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID_P, kk ? 1u : 0u);
 #pragma unroll
-        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(t_lo + kk * 2048, 16, 1024), ID, 1u);
+        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + TILE + kk * 2048, 16, 1024), ID_P, 1u);
 #pragma unroll
-        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(t_hi + kk * 2048, 16, 1024), ID, 1u);
+        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID_P, 1u);
         tc_commit(&done);
     }
+    __syncwarp();
     WAIT(&done, 1);
     tc_fence_after();
-    if (warp >= 2) {
+    if (row < D) {      // Y where K and P were
+        uint32_t r[32];
+        tmem_ld32(row_addr + 64, r);
+        tc_wait_ld();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint32_t r[32];
-            tmem_ld32(row_addr + 32 * half, r);
-            tc_wait_ld();
+        for (int i = 0; i < 4; ++i) {
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float2 x = unpack_bf16(pw[16 * half + i]), y = unpack_bf16(pl[16 * half + i]);
-                const int s = 32 * half + 2 * i;
-                pw[16 * half + i] = pack_bf16(fmaf(x.x + y.x, sbeta[s], __uint_as_float(r[2 * i])), fmaf(x.y + y.y, sbeta[s + 1], __uint_as_float(r[2 * i + 1])));
-            }
+            for (int e = 0; e < 4; ++e) split2(__uint_as_float(r[8 * i + 2 * e]), __uint_as_float(r[8 * i + 2 * e + 1]), hi[e], lo[e]);
+            const int at16 = row * 128 + (((4 * part + i) ^ (row & 7)) << 4);
+            *reinterpret_cast<uint4*>(sm + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(sm + Out::Y + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(sm + PREP_P + j * 128 + ((i ^ (j & 7)) << 4)) = make_uint4(pw[4 * i], pw[4 * i + 1], pw[4 * i + 2], pw[4 * i + 3]);
-        fence_proxy_async_smem();
     }
+    if (is_p) {         // P T where T was
+        uint32_t r[32];
+        tmem_ld32(row_addr, r);
+        tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__uint_as_float(r[8 * i + 2 * e]), __uint_as_float(r[8 * i + 2 * e + 1]));
+            *reinterpret_cast<uint4*>(work + PREP_T + j * 128 + (((4 * part + i) ^ (j & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
     if (tid == 0) {
-        bulk_store(tp.ws + ((size_t)at * p.H + h) * CHUNK_BYTES, sm + PREP_T_HI, CHUNK_BYTES);
+        uint8_t* to = tp.ws + ((size_t)at * p.H + h) * Out::BYTES;
+        bulk_store(to, sm, 2 * Out::Y);
+        bulk_store(to + Out::PT, work + PREP_T, TILE);
+        bulk_store(to + Out::META, sm + L::META, 2 * DC * 4);
         bulk_commit();
         bulk_wait_all();
     }
     settle_after_timeout(abortp);
-    if (warp == 1) tmem_dealloc(tb, 64);
+    if (warp == 1) tmem_dealloc(tb, 128);
 }
 
 // ------------------------------------------------------------------------------------------------ the walk over a sequence's chunks
-// Six warps: 0 loads, 1 issues the MMAs, 2..5 are the four lane quadrants.  With W = 32 columns of d_v, per chunk:
-//   [K; Q] [S_hi | S_lo]        128 x 64 x d    lanes 0..63 K S, 64..127 Q S
-//   [T_hi; P T] [R_hi | R_lo]   128 x 64 x 64   and T_lo R_hi 128 x 32 x 64 beside it
-//   K^T [U_hi | U_lo]           128 x 64 x 64   lanes d_k, K as the MN-major operand
-// The state is 32 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R and U, 2 and 3 the outputs meanwhile.
-constexpr int WALK_THREADS = 6 * 32, W = 32;
-constexpr uint32_t COL_X = 0, COL_U = 64, COL_UL = 128, COL_D = 160, WALK_COLS = 256;
+// Warps 4..11 work on rows, two for each lane quadrant (16 columns each); 2 issues the MMAs and 3 loads (on the schedulers of the quadrants that make the
+// outputs, off the chain; 0 and 1 do nothing).  With W = 32 columns of d_v, per chunk:
+//   [K; Q] [S_hi | S_lo]          128 x 64 x d    lanes 0..63 K S, 64..127 Q S
+//   (Y_hi + Y_lo) [R_hi | R_lo]   128 x 64 x 64   lanes d_k; on the chain
+//   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
+// The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
+// runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
+constexpr int WALK_THREADS = 12 * 32, W = 32, WC = 16;
+constexpr uint32_t COL_X = 0, COL_D = 64, COL_O = 128, WALK_COLS = 256;
 
-template <int D>
+template <int D, int ST>
 struct Walk {
-    static constexpr int KQ = 2 * TILE * (D / 64), STAGE = KQ + ((CHUNK_BYTES + 1023) & ~1023), STAGES = 2;
-    static constexpr int OFF_S = STAGES * STAGE, OFF_R = OFF_S + D * 128, OFF_U = OFF_R + TILE, SMEM = OFF_U + TILE + 1024;
-    static constexpr uint32_t LOAD_BYTES = KQ + CHUNK_BYTES;
+    using In = Chunk<D>;
+    static constexpr int STAGES = ST;
+    static constexpr int KQ = 2 * TILE * (D / 64), Y = KQ, V = Y + ((In::BYTES + 1023) & ~1023), STAGE = V + DC * W * 2;
+    static constexpr int OFF_S = STAGES * STAGE, OFF_R = OFF_S + D * 128, OFF_O = OFF_R + TILE, SMEM = OFF_O + 4 * 1024 + 1024;
+    static constexpr uint32_t Y_BYTES = In::BYTES + DC * W * 2;
 };
 
-template <int D>
-__global__ void __launch_bounds__(WALK_THREADS) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const DeltaTcParams tp) {
-    using L = Walk<D>;
+// A wait on the chain of dependent steps: polls, so the thread goes on as soon as the barrier flips, before it parks.
+__device__ __forceinline__ void wait_hot(uint64_t* bar, uint32_t parity, volatile int* abortp, int* status) {
+#pragma unroll 1
+    for (int i = 0; i < 512; ++i)
+        if (mbar_test_wait_t<false>(bar, parity)) return;
+    mbar_wait_slow<false>(bar, parity, abortp, status, MBAR_WAIT_LIMIT);
+}
+#define WAIT_HOT(bar, parity) wait_hot(bar, parity, abortp, p.status)
+
+// 16 fp32 values (pairs) in two bf16 terms into row r of an operand whose rows hold [32 high | 32 low]; piece: 0 or 2 (16-byte pieces).
+__device__ __forceinline__ void put_split(uint8_t* tile, int r, int piece, const uint64_t (&x)[WC / 2]) {
+    uint8_t* row = tile + r * 128;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 y = unpair(x[4 * i + e]);
+            h[e] = pack_bf16(y.x, y.y);
+            const float2 z = unpair(add2(x[4 * i + e], pair((h[e] << 16) ^ 0x80000000u, (h[e] & 0xffff0000u) ^ 0x80000000u)));
+            l[e] = pack_bf16(z.x, z.y);
+        }
+        *reinterpret_cast<uint4*>(row + (((piece + i) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(row + (((piece + i + 4) ^ (r & 7)) << 4)) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+}
+
+template <int D, int ST>
+__global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
+                                                                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
+    using L = Walk<D, ST>;
+    using In = Chunk<D>;
     constexpr int SLABS = D / W;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full[L::STAGES], empty[L::STAGES], s_ready, r_ready, u_ready, x_full, u_full, d_full;
+    __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], s_ready, r_ready, x_full, d_full, o_full, o_free;
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
@@ -331,17 +535,22 @@ __global__ void __launch_bounds__(WALK_THREADS) delta_walk_kernel(const __grid_c
     const int slab = blockIdx.x % SLABS, h = (blockIdx.x / SLABS) % p.H, n = blockIdx.x / (SLABS * p.H);
 
     if (tid == 0) {
-        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-        mbar_init(&s_ready, 4);
-        mbar_init(&r_ready, 2);
-        mbar_init(&u_ready, 2);
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&kq_full[i], 1);
+            mbar_init(&kq_empty[i], 1);
+            mbar_init(&y_full[i], 1);
+            mbar_init(&y_empty[i], 5);      // the MMAs, and the four warps that read the gates off the chain
+        }
+        mbar_init(&s_ready, 8);
+        mbar_init(&r_ready, 4);
         mbar_init(&x_full, 1);
-        mbar_init(&u_full, 1);
         mbar_init(&d_full, 1);
+        mbar_init(&o_full, 1);
+        mbar_init(&o_free, 4);
         abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 1) { tmem_alloc(&tmem_base, WALK_COLS); tmem_relinquish(); }
+    if (warp == 2) { tmem_alloc(&tmem_base, WALK_COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -354,185 +563,192 @@ __global__ void __launch_bounds__(WALK_THREADS) delta_walk_kernel(const __grid_c
     const bool work = slot >= 0 && slot < p.num_slots && (len > 0 || !p.use_initial_state);
     const int nc = work && len > 0 ? (len + DC - 1) / DC : 0;
 
-    if (warp == 0) {
-        if (lane == 0) {
-            if (nc > 0) { prefetch_tensormap(&map_k); prefetch_tensormap(&map_q); }
+    if (warp == 3) {
+        if (lane == 0 && nc > 0) {
+            prefetch_tensormap(&map_k);
+            prefetch_tensormap(&map_q);
+            prefetch_tensormap(&map_v);
+            prefetch_tensormap(&map_o);
             const int hq = h / p.group;
             for (int c = 0; c < nc && !*abortp; ++c) {
-                const int st = c % L::STAGES;
-                if (c >= L::STAGES) WAIT(&empty[st], (c / L::STAGES - 1) & 1);
+                const int st = c % ST;
                 uint8_t* to = sm + st * L::STAGE;
-                mbar_arrive_expect_tx(&full[st], L::LOAD_BYTES);
+                if (c >= ST) WAIT(&kq_empty[st], (c / ST - 1) & 1);
+                mbar_arrive_expect_tx(&kq_full[st], L::KQ);
                 for (int half = 0; half < D / 64; ++half) {
-                    tma_load_4d(to + half * 2 * TILE, &map_k, &full[st], 0, t_begin + c * DC, half, hq);
-                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &full[st], 0, t_begin + c * DC, half, hq);
+                    tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[st], 0, t_begin + c * DC, half, hq);
+                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[st], 0, t_begin + c * DC, half, hq);
                 }
-                bulk_load(to + L::KQ, tp.ws + ((size_t)(first + c) * p.H + h) * CHUNK_BYTES, CHUNK_BYTES, &full[st]);
+                if (c >= ST) WAIT(&y_empty[st], (c / ST - 1) & 1);
+                mbar_arrive_expect_tx(&y_full[st], L::Y_BYTES);
+                bulk_load(to + L::Y, tp.ws + ((size_t)(first + c) * p.H + h) * In::BYTES, In::BYTES, &y_full[st]);
+                tma_load_3d(to + L::V, &map_v, &y_full[st], slab * W, h, t_begin + c * DC);
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == 2) {
         if (elect_one()) {
-            const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R, u_at = base + L::OFF_U;
-            constexpr uint32_t ID_64 = idesc_bf16(128, 64, 0, 1), ID_32 = idesc_bf16(128, 32, 0, 1), ID_KT = idesc_bf16(128, 64, 1, 1);
+            const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
+            constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
             for (int c = 0; c < nc; ++c) {
-                const int st = c % L::STAGES;
-                const uint32_t kq = base + st * L::STAGE, ch = kq + L::KQ;
-                WAIT(&full[st], (c / L::STAGES) & 1);
-                WAIT(&s_ready, c & 1);
+                const int st = c % ST;
+                const uint32_t kq = base + st * L::STAGE, y = kq + L::Y;
+                WAIT_HOT(&kq_full[st], (c / ST) & 1);
+                WAIT_HOT(&s_ready, c & 1);
                 tc_fence_after();
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    mma_ss(tb + COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, 16, 1024), ID_64, kk ? 1u : 0u);
+                    mma_ss(tb + COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&x_full);
-                WAIT(&r_ready, c & 1);
+                tc_commit(&kq_empty[st]);
+                WAIT_HOT(&y_full[st], (c / ST) & 1);
+                WAIT_HOT(&r_ready, c & 1);
                 tc_fence_after();
 #pragma unroll
-                for (int kk = 0; kk < DC / 16; ++kk)
-                    mma_ss(tb + COL_U, smem_desc_sw128(ch + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID_64, kk ? 1u : 0u);
+                for (int k = 1; k >= 0; --k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
 #pragma unroll
-                for (int kk = 0; kk < DC / 16; ++kk)      // rows 64..127 are whatever lies behind T_lo: their lanes are not read
-                    mma_ss(tb + COL_UL, smem_desc_sw128(ch + 2 * TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID_32, kk ? 1u : 0u);
-                tc_commit(&u_full);
-                WAIT(&u_ready, c & 1);
-                tc_fence_after();
-#pragma unroll
-                for (int kk = 0; kk < DC / 16; ++kk)      // d = 64: lanes 64..127 multiply what lies behind K and Q and are not read
-                    mma_ss(tb + COL_D, smem_desc_sw128(kq + kk * 2048, 2 * TILE, 1024), smem_desc_sw128(u_at + kk * 2048, 16, 1024), ID_KT, kk ? 1u : 0u);
+                    for (int kk = 0; kk < DC / 16; ++kk)
+                        mma_ss(tb + COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID, !k || kk ? 1u : 0u);
                 tc_commit(&d_full);
-                tc_commit(&empty[st]);
+                if (c > 0) {
+                    WAIT_HOT(&o_free, (c - 1) & 1);
+                    tc_fence_after();
+                }
+#pragma unroll
+                for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
+                    mma_ss(tb + COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
+                tc_commit(&o_full);
+                tc_commit(&y_empty[st]);
             }
         }
-    } else if (work) {
-        const int quad = warp & 3, row = 32 * quad + lane;      // lane of TMEM: d_k of the state; token (quadrants 0, 1: of R and U, 2, 3: of the outputs)
-        const uint32_t lane_addr = tb + ((uint32_t)(32 * quad) << 16);
-        const bool has_state = row < D, first_half = quad < 2;
+    } else if (warp >= 4 && work) {
+        const int quad = warp & 3, row = 32 * quad + lane;      // lane of TMEM: d_k of the state; token (quadrants 0, 1: of R, 2, 3: of the outputs)
+        const int part = (warp - 4) >> 2, piece = 2 * part;     // which 16 of the 32 columns
+        const uint32_t lane_addr = tb + ((uint32_t)(32 * quad) << 16) + WC * part;
+        const bool has_state = row < D, makes_r = quad < 2;
         const int j = row & 63;
-        float* S = p.state + (((size_t)slot * p.H + h) * D + row) * D + slab * W;
-        const size_t tok_stride = (size_t)p.H * D;
-        const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v) + ((size_t)t_begin * p.H + h) * D + slab * W;
-        __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)t_begin * p.H + h) * D + slab * W;
-        float s[W];
+        float* S = p.state + (((size_t)slot * p.H + h) * D + row) * D + slab * W + WC * part;
+        uint64_t s[WC / 2], y[WC / 2];
 #pragma unroll
-        for (int i = 0; i < W; i += 4) {
+        for (int i = 0; i < WC; i += 4) {
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
             if (has_state && p.use_initial_state) x = *reinterpret_cast<const float4*>(S + i);
-            s[i] = x.x; s[i + 1] = x.y; s[i + 2] = x.z; s[i + 3] = x.w;
+            s[i / 2] = pair(x.x, x.y);
+            s[i / 2 + 1] = pair(x.z, x.w);
+            y[i / 2] = y[i / 2 + 1] = 0;
         }
-        uint4 vr[4];
-        auto fetch_v = [&](int c) {
-            const int t = c * DC + j;
+        // The outputs of chunk c (quadrants 2, 3): y, scaled, and P T R.  Whole rows of 32 tokens leave by a TMA store of this warp; the stores of a ragged end
+        // come from the registers.
+        uint8_t* o_tile = sm + L::OFF_O + ((quad & 1) * 2 + part) * 1024;
+        auto outputs = [&](int c) {
+            uint32_t a[WC], b[WC];
+            WAIT_HOT(&o_full, c & 1);
+            tc_fence_after();
+            tmem_ld16(lane_addr + COL_O, a);
+            tmem_ld16(lane_addr + COL_O + 32, b);
+            tc_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&o_free);
+            uint32_t x[WC / 2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vr[i] = t < len ? __ldg(reinterpret_cast<const uint4*>(v + (size_t)t * tok_stride) + i) : make_uint4(0u, 0u, 0u, 0u);
-        };
-        if (first_half && nc > 0) fetch_v(0);
-        for (int c = 0; c < nc; ++c) {
-            const int st = c % L::STAGES, live = min(DC, len - c * DC);
-            const float* meta = reinterpret_cast<const float*>(sm + st * L::STAGE + L::KQ + CHUNK_TILES);
-            if (has_state) put_split(sm + L::OFF_S, row, s);
-            WAIT(&full[st], (c / L::STAGES) & 1);
-            if (live < DC) {
-                // rows of K behind the sequence's end meet a U of zero: whatever they hold must be finite
-                for (int i = live * 8 + (tid - 64); i < DC * 8; i += 128)
-#pragma unroll
-                    for (int half = 0; half < D / 64; ++half) *reinterpret_cast<uint4*>(sm + st * L::STAGE + half * 2 * TILE + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < WC / 2; ++i) {
+                const float2 z = unpair(add2(y[i], add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1]))));
+                x[i] = pack_bf16(z.x, z.y);
             }
-            // (read ahead of the arrival: nothing of the stage is touched by a warp that the others may have left behind)
-            const float G = meta[DC + j], sG = meta[j], last = meta[2 * DC - 1], beta = meta[2 * DC + j], w = meta[3 * DC + j];
+            const int t0 = c * DC + 32 * (quad & 1);      // this warp's first token
+            if (t0 + 32 <= len) {
+                if (lane == 0) bulk_wait_read();
+                __syncwarp();
+                *reinterpret_cast<uint4*>(o_tile + lane * 32) = make_uint4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<uint4*>(o_tile + lane * 32 + 16) = make_uint4(x[4], x[5], x[6], x[7]);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_3d(&map_o, o_tile, slab * W + WC * part, h, t_begin + t0);
+                    bulk_commit();
+                }
+            } else if (t0 + lane < len) {
+                uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(t_begin + t0 + lane) * p.H + h) * D + slab * W + WC * part);
+                to[0] = make_uint4(x[0], x[1], x[2], x[3]);
+                to[1] = make_uint4(x[4], x[5], x[6], x[7]);
+            }
+        };
+        for (int c = 0; c < nc; ++c) {
+            const int st = c % ST, live = min(DC, len - c * DC);
+            uint8_t* stage = sm + st * L::STAGE;
+            const float* meta = reinterpret_cast<const float*>(stage + L::Y + In::META);
+            uint32_t a[WC], b[WC];
+            float last;
+            if (has_state) put_split(sm + L::OFF_S, row, piece, s);
             fence_proxy_async_smem();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&s_ready);
-            if (first_half) {
-                float r[W];
-                uint32_t a[32];
-                WAIT(&x_full, c & 1);
+            if (makes_r) {
+                WAIT_HOT(&y_full[st], (c / ST) & 1);
+                last = meta[2 * DC - 1];
+                const float G = -meta[DC + j];
+                uint4 vr[2];
+                vr[0] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + part * 32);
+                vr[1] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + part * 32 + 16);
+                WAIT_HOT(&x_full, c & 1);
                 tc_fence_after();
-                tmem_ld32(lane_addr + COL_X, a);
+                tmem_ld16(lane_addr + COL_X, a);
+                tmem_ld16(lane_addr + COL_X + 32, b);
                 tc_wait_ld();
+                uint64_t r[WC / 2];
 #pragma unroll
-                for (int i = 0; i < W; ++i) r[i] = __uint_as_float(a[i]);
-                tmem_ld32(lane_addr + COL_X + 32, a);
-                tc_wait_ld();
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const uint32_t word = reinterpret_cast<const uint32_t*>(vr)[i / 2];
-                    const float x = __uint_as_float(i & 1 ? word & 0xffff0000u : word << 16);
-                    r[i] = j < live ? fmaf(-G, r[i] + __uint_as_float(a[i]), x) : 0.f;
+                for (int i = 0; i < WC / 2; ++i) {
+                    const uint32_t word = reinterpret_cast<const uint32_t*>(vr)[i];
+                    r[i] = fma2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])), pair(word << 16, word & 0xffff0000u));
                 }
-                put_split(sm + L::OFF_R, j, r);
+                if (j >= live) {      // a token behind the sequence's end, whatever it holds
+#pragma unroll
+                    for (int i = 0; i < WC / 2; ++i) r[i] = 0;
+                }
+                put_split(sm + L::OFF_R, j, piece, r);
                 fence_proxy_async_smem();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&r_ready);
-                if (c + 1 < nc) fetch_v(c + 1);
-                WAIT(&u_full, c & 1);
-                tc_fence_after();
-                tmem_ld32(lane_addr + COL_UL, a);
-                tc_wait_ld();
-#pragma unroll
-                for (int i = 0; i < W; ++i) r[i] = fmaf(beta, r[i], __uint_as_float(a[i]));
-                tmem_ld32(lane_addr + COL_U + 32, a);
-                tc_wait_ld();
-#pragma unroll
-                for (int i = 0; i < W; ++i) r[i] += __uint_as_float(a[i]);
-                tmem_ld32(lane_addr + COL_U, a);
-                tc_wait_ld();
-#pragma unroll
-                for (int i = 0; i < W; ++i) r[i] = w * (r[i] + __uint_as_float(a[i]));
-                put_split(sm + L::OFF_U, j, r);
-                fence_proxy_async_smem();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&u_ready);
             } else {
-                float y[W];
-                uint32_t a[32];
-                WAIT(&x_full, c & 1);
+                if (c > 0) outputs(c - 1);
+                WAIT_HOT(&y_full[st], (c / ST) & 1);
+                last = meta[2 * DC - 1];
+                const float G = meta[j];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&y_empty[st]);
+                WAIT_HOT(&x_full, c & 1);
                 tc_fence_after();
-                tmem_ld32(lane_addr + COL_X, a);
+                tmem_ld16(lane_addr + COL_X, a);
+                tmem_ld16(lane_addr + COL_X + 32, b);
                 tc_wait_ld();
 #pragma unroll
-                for (int i = 0; i < W; ++i) y[i] = sG * __uint_as_float(a[i]);
-                WAIT(&u_full, c & 1);
-                tc_fence_after();
-                tmem_ld32(lane_addr + COL_U, a);
-                tc_wait_ld();
-                const int t = c * DC + j;
-                if (j < live) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t x[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[e] = pack_bf16(y[8 * i + 2 * e] + __uint_as_float(a[8 * i + 2 * e]), y[8 * i + 2 * e + 1] + __uint_as_float(a[8 * i + 2 * e + 1]));
-                        *(reinterpret_cast<uint4*>(o + (size_t)t * tok_stride) + i) = make_uint4(x[0], x[1], x[2], x[3]);
-                    }
-                }
+                for (int i = 0; i < WC / 2; ++i) y[i] = mul2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
             }
-            WAIT(&d_full, c & 1);
+            WAIT_HOT(&d_full, c & 1);
             tc_fence_after();
-            {
-                uint32_t a[32];
-                tmem_ld32(lane_addr + COL_D + 32, a);
-                tc_wait_ld();
-                float low[W];
+            tmem_ld16(lane_addr + COL_D, a);
+            tmem_ld16(lane_addr + COL_D + 32, b);
+            tc_wait_ld();
+            const uint64_t keep = pair(last, last);
 #pragma unroll
-                for (int i = 0; i < W; ++i) low[i] = __uint_as_float(a[i]);
-                tmem_ld32(lane_addr + COL_D, a);
-                tc_wait_ld();
-#pragma unroll
-                for (int i = 0; i < W; ++i) s[i] = fmaf(last, s[i], low[i] + __uint_as_float(a[i]));
-            }
+            for (int i = 0; i < WC / 2; ++i) s[i] = fma2(keep, s[i], add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
         }
+        if (!makes_r && nc > 0) outputs(nc - 1);
         if (has_state) {
 #pragma unroll
-            for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(S + i) = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
+            for (int i = 0; i < WC; i += 4) {
+                const float2 x = unpair(s[i / 2]), z = unpair(s[i / 2 + 1]);
+                *reinterpret_cast<float4*>(S + i) = make_float4(x.x, x.y, z.x, z.y);
+            }
         }
+        if (lane == 0) bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
     settle_after_timeout(abortp);
-    if (warp == 1) tmem_dealloc(tb, WALK_COLS);
+    if (warp == 2) tmem_dealloc(tb, WALK_COLS);
 }
 
 // [T_total, H_qk, D] bf16 as (64 elements, t, part of a row, head); a box is 64 tokens of one part, one swizzled tile.
@@ -543,20 +759,37 @@ bool make_map(CUtensorMap* m, const void* base, int T_total, int H, int d) {
     return encode_tile_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+// [T_total, H, D] bf16 as (element, head, t); a box is `columns` elements of `tokens` tokens, packed rows.
+bool make_slab_map(CUtensorMap* m, const void* base, int T_total, int H, int d, int columns, int tokens) {
+    cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)T_total};
+    cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)H * d * 2};
+    cuuint32_t box[3] = {(cuuint32_t)columns, 1, (cuuint32_t)tokens};
+    return encode_tile_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
 long long chunk_slots(const dsla_delta_prefill_args* a) {
     return a->cu_seqlens ? (long long)a->T_total / DC + a->N : (long long)a->N * ((a->T + DC - 1) / DC);
+}
+
+template <int D, int ST>
+dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CUtensorMap& mq, const CUtensorMap& mv, const CUtensorMap& mo, const DeltaTcParams& tp) {
+    if (cudaFuncSetAttribute(delta_walk_kernel<D, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, Walk<D, ST>::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
+    cfg.blockDim = dim3(WALK_THREADS);
+    cfg.dynamicSmemBytes = Walk<D, ST>::SMEM;
+    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D, ST>, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
+    count_launch();
+    return DSLA_OK;
 }
 
 template <int D>
 dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cudaStream_t s) {
     const DeltaParams& p = tp.p;
-    CUtensorMap mk{}, mq{};
-    if (a->T_total > 0 && (!make_map(&mk, p.k, a->T_total, a->H_qk, D) || !make_map(&mq, p.q, a->T_total, a->H_qk, D))) return DSLA_ERR_CUDA;
+    CUtensorMap mk{}, mq{}, mv{}, mo{};
+    if (a->T_total > 0 && (!make_map(&mk, p.k, a->T_total, a->H_qk, D) || !make_map(&mq, p.q, a->T_total, a->H_qk, D) ||
+                           !make_slab_map(&mv, p.v, a->T_total, p.H, D, W, DC) || !make_slab_map(&mo, p.o, a->T_total, p.H, D, WC, 32)))
+        return DSLA_ERR_CUDA;
     const long long prep = a->T_total > 0 ? (long long)tp.slots * p.H : 0, walk = (long long)p.N * p.H * (D / W);
     if (prep > 0x7fffffffLL || walk > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(delta_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PREP_SMEM) != cudaSuccess ||
-        cudaFuncSetAttribute(delta_walk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Walk<D>::SMEM) != cudaSuccess)
-        return DSLA_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -565,23 +798,24 @@ dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cu
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (prep > 0) {
+        if (cudaFuncSetAttribute(delta_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Prep<D>::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
         cfg.gridDim = dim3((unsigned)prep);
         cfg.blockDim = dim3(PREP_THREADS);
-        cfg.dynamicSmemBytes = PREP_SMEM;
+        cfg.dynamicSmemBytes = Prep<D>::SMEM;
         if (cudaLaunchKernelEx(&cfg, delta_chunk_kernel<D>, mk, mq, tp) != cudaSuccess) return DSLA_ERR_CUDA;
         count_launch();
     }
     cfg.gridDim = dim3((unsigned)walk);
-    cfg.blockDim = dim3(WALK_THREADS);
-    cfg.dynamicSmemBytes = Walk<D>::SMEM;
-    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D>, mk, mq, tp) != cudaSuccess) return DSLA_ERR_CUDA;
-    count_launch();
+    const dsla_status rc = walk <= sm_count() ? launch_walk<D, 2>(cfg, mk, mq, mv, mo, tp) : launch_walk<D, 1>(cfg, mk, mq, mv, mo, tp);
+    if (rc != DSLA_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? DSLA_OK : DSLA_ERR_CUDA;
 }
 
 }  // namespace
 
-size_t delta_tc_workspace_bytes(const dsla_delta_prefill_args* a) { return a->T_total > 0 ? (size_t)chunk_slots(a) * a->H * CHUNK_BYTES : 0; }
+size_t delta_tc_workspace_bytes(const dsla_delta_prefill_args* a) {
+    return a->T_total > 0 ? (size_t)chunk_slots(a) * a->H * (a->d_k == 128 ? Chunk<128>::BYTES : Chunk<64>::BYTES) : 0;
+}
 
 dsla_status launch_delta_tc(const DeltaParams& p, const dsla_delta_prefill_args* a, cudaStream_t s) {
     const long long slots = chunk_slots(a);
