@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
     __syncthreads();
     tc_fence_after();
     const uint32_t tb = tmem_base;
-    if (tid == 0) {
+    if (warp == 0 && elect_one()) {
         WAIT(&full, 0);
         tc_fence_after();
         const uint32_t kq = smem_u32(sm);
@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
     }
     fence_proxy_async_smem();
     __syncthreads();
-    if (tid == 0) {
+    if (warp == 0 && elect_one()) {
         tc_fence_after();
         const uint32_t kt = smem_u32(sm), tt = smem_u32(work + PREP_T), wt = smem_u32(work + PREP_W);
         // Y: d = 64 has 64 rows, the other half of the product is not read
@@ -465,21 +465,21 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
         bulk_store(to + Out::PT, work + PREP_T, TILE);
         bulk_store(to + Out::META, sm + L::META, 2 * DC * 4);
         bulk_commit();
-        bulk_wait_all();
+        bulk_wait_read();
     }
     settle_after_timeout(abortp);
     if (warp == 1) tmem_dealloc(tb, 128);
 }
 
 // ------------------------------------------------------------------------------------------------ the walk over a sequence's chunks
-// Warps 4..11 work on rows, two for each lane quadrant (16 columns each); 2 issues the MMAs and 3 loads (on the schedulers of the quadrants that make the
-// outputs, off the chain; 0 and 1 do nothing).  With W = 32 columns of d_v, per chunk:
+// Warps 0..7 work on rows, two for each lane quadrant (16 columns each), 8 issues the MMAs, 9 loads.  (Issued by a row warp the MMAs hold up that warp's rows: 2750
+// cycles per chunk instead of 2450.)  With W = 32 columns of d_v, per chunk:
 //   [K; Q] [S_hi | S_lo]          128 x 64 x d    lanes 0..63 K S, 64..127 Q S
 //   (Y_hi + Y_lo) [R_hi | R_lo]   128 x 64 x 64   lanes d_k; on the chain
 //   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-constexpr int WALK_THREADS = 12 * 32, W = 32, WC = 16;
+constexpr int WALK_THREADS = 10 * 32, W = 32, WC = 16;
 constexpr uint32_t COL_X = 0, COL_D = 64, COL_O = 128, WALK_COLS = 256;
 
 template <int D, int ST>
@@ -499,6 +499,11 @@ __device__ __forceinline__ void wait_hot(uint64_t* bar, uint32_t parity, volatil
     mbar_wait_slow<false>(bar, parity, abortp, status, MBAR_WAIT_LIMIT);
 }
 #define WAIT_HOT(bar, parity) wait_hot(bar, parity, abortp, p.status)
+// Rows to the MMA warp, through named barriers: eight warps and four arrive, it alone waits.  (Every wait before an arrival is bounded, so each arrives.)
+#define S_READY_SYNC() asm volatile("bar.sync 1, 288;" ::: "memory")
+#define S_READY_ARRIVE() asm volatile("bar.arrive 1, 288;" ::: "memory")
+#define R_READY_SYNC() asm volatile("bar.sync 2, 160;" ::: "memory")
+#define R_READY_ARRIVE() asm volatile("bar.arrive 2, 160;" ::: "memory")
 
 // 16 fp32 values (pairs) in two bf16 terms into row r of an operand whose rows hold [32 high | 32 low]; piece: 0 or 2 (16-byte pieces).
 __device__ __forceinline__ void put_split(uint8_t* tile, int r, int piece, const uint64_t (&x)[WC / 2]) {
@@ -525,7 +530,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
     using In = Chunk<D>;
     constexpr int SLABS = D / W;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], s_ready, r_ready, x_full, d_full, o_full, o_free;
+    __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free;
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
@@ -541,8 +546,6 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
             mbar_init(&y_full[i], 1);
             mbar_init(&y_empty[i], 5);      // the MMAs, and the four warps that read the gates off the chain
         }
-        mbar_init(&s_ready, 8);
-        mbar_init(&r_ready, 4);
         mbar_init(&x_full, 1);
         mbar_init(&d_full, 1);
         mbar_init(&o_full, 1);
@@ -550,7 +553,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
         abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 2) { tmem_alloc(&tmem_base, WALK_COLS); tmem_relinquish(); }
+    if (warp == 8) { tmem_alloc(&tmem_base, WALK_COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -563,7 +566,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
     const bool work = slot >= 0 && slot < p.num_slots && (len > 0 || !p.use_initial_state);
     const int nc = work && len > 0 ? (len + DC - 1) / DC : 0;
 
-    if (warp == 3) {
+    if (warp == 9) {
         if (lane == 0 && nc > 0) {
             prefetch_tensormap(&map_k);
             prefetch_tensormap(&map_q);
@@ -585,44 +588,45 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
                 tma_load_3d(to + L::V, &map_v, &y_full[st], slab * W, h, t_begin + c * DC);
             }
         }
-    } else if (warp == 2) {
-        if (elect_one()) {
-            const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
-            constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
-            for (int c = 0; c < nc; ++c) {
-                const int st = c % ST;
-                const uint32_t kq = base + st * L::STAGE, y = kq + L::Y;
-                WAIT_HOT(&kq_full[st], (c / ST) & 1);
-                WAIT_HOT(&s_ready, c & 1);
-                tc_fence_after();
+    } else if (warp == 8) {
+        const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
+        constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
+        for (int c = 0; c < nc; ++c) {
+            const int st = c % ST;
+            const uint32_t kq = base + st * L::STAGE, y = kq + L::Y;
+            WAIT(&kq_full[st], (c / ST) & 1);
+            S_READY_SYNC();
+            tc_fence_after();
+            if (elect_one()) {
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
                     mma_ss(tb + COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&x_full);
                 tc_commit(&kq_empty[st]);
-                WAIT_HOT(&y_full[st], (c / ST) & 1);
-                WAIT_HOT(&r_ready, c & 1);
-                tc_fence_after();
+            }
+            __syncwarp();
+            WAIT(&y_full[st], (c / ST) & 1);
+            if (c > 0) WAIT(&o_free, (c - 1) & 1);
+            R_READY_SYNC();
+            tc_fence_after();
+            if (elect_one()) {
 #pragma unroll
                 for (int k = 1; k >= 0; --k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
 #pragma unroll
                     for (int kk = 0; kk < DC / 16; ++kk)
                         mma_ss(tb + COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID, !k || kk ? 1u : 0u);
                 tc_commit(&d_full);
-                if (c > 0) {
-                    WAIT_HOT(&o_free, (c - 1) & 1);
-                    tc_fence_after();
-                }
 #pragma unroll
                 for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
                     mma_ss(tb + COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&o_full);
                 tc_commit(&y_empty[st]);
             }
+            __syncwarp();
         }
-    } else if (warp >= 4 && work) {
+    } else if (work) {
         const int quad = warp & 3, row = 32 * quad + lane;      // lane of TMEM: d_k of the state; token (quadrants 0, 1: of R, 2, 3: of the outputs)
-        const int part = (warp - 4) >> 2, piece = 2 * part;     // which 16 of the 32 columns
+        const int part = warp >> 2, piece = 2 * part;     // which 16 of the 32 columns
         const uint32_t lane_addr = tb + ((uint32_t)(32 * quad) << 16) + WC * part;
         const bool has_state = row < D, makes_r = quad < 2;
         const int j = row & 63;
@@ -682,8 +686,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
             if (has_state) put_split(sm + L::OFF_S, row, piece, s);
             fence_proxy_async_smem();
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s_ready);
+            S_READY_ARRIVE();
             if (makes_r) {
                 WAIT_HOT(&y_full[st], (c / ST) & 1);
                 last = meta[2 * DC - 1];
@@ -709,8 +712,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
                 put_split(sm + L::OFF_R, j, piece, r);
                 fence_proxy_async_smem();
                 tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&r_ready);
+                R_READY_ARRIVE();
             } else {
                 if (c > 0) outputs(c - 1);
                 WAIT_HOT(&y_full[st], (c / ST) & 1);
@@ -743,12 +745,12 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
                 *reinterpret_cast<float4*>(S + i) = make_float4(x.x, x.y, z.x, z.y);
             }
         }
-        if (lane == 0) bulk_wait_all();
+        if (lane == 0) bulk_wait_read();
     }
     tc_fence_before();
     __syncthreads();
     settle_after_timeout(abortp);
-    if (warp == 2) tmem_dealloc(tb, WALK_COLS);
+    if (warp == 8) tmem_dealloc(tb, WALK_COLS);
 }
 
 // [T_total, H_qk, D] bf16 as (64 elements, t, part of a row, head); a box is 64 tokens of one part, one swizzled tile.
