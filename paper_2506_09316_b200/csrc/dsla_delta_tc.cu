@@ -11,6 +11,7 @@
 // Y is made of), with fp32 sums; (I + A)^-1 is fp32.  The state itself stays in fp32 registers and each chunk adds one tensor-core sum to
 // it, with rounding.  P T, which reaches only the bf16 output, has one term.
 #include <cuda.h>
+#include <cstdlib>
 
 #include "dsla_internal.cuh"
 #include "tc_utils.cuh"
@@ -133,16 +134,19 @@ __device__ __forceinline__ void tf32_terms(float x, uint32_t& hi, uint32_t& lo) 
     lo = __float_as_uint(x - __uint_as_float(hi));
 }
 // c[m tile] += M[16 MT x 8 KT] B[8 KT x 8], both in shared memory (row pitches pa, pb), as products of two TF32 terms.
-template <int MT, int KT>
-__device__ __forceinline__ void product(float (&c)[MT][4], const float* M, int pa, const float* B, int pb, int lane) {
+// Steps of 8 before k_first meet zeros of B; with LOWER, M is lower triangular.
+template <int MT, int KT, bool LOWER>
+__device__ __forceinline__ void product(float (&c)[MT][4], const float* M, int pa, const float* B, int pb, int k_first, int lane) {
     const int r = lane >> 2, q = lane & 3;
 #pragma unroll
     for (int k = 0; k < KT; ++k) {
+        if (k < k_first) continue;
         uint32_t bh[2], bl[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) tf32_terms(B[(8 * k + q + 4 * i) * pb + r], bh[i], bl[i]);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+            if (LOWER && 2 * m + 1 < k) continue;
             uint32_t ah[4], al[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) tf32_terms(M[(16 * m + r + 8 * (i & 1)) * pa + 8 * k + q + 4 * (i >> 1)], ah[i], al[i]);
@@ -158,7 +162,7 @@ __device__ __forceinline__ void lower_left(const float* A, float* X, float* scra
     float c[MT][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m) c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0.f;
-    product<MT, 2 * MT>(c, A + r0 * XP + c0, XP, X + c0 * XP + c0 + n0, XP, lane);
+    product<MT, 2 * MT, false>(c, A + r0 * XP + c0, XP, X + c0 * XP + c0 + n0, XP, n0 / 8, lane);
     const int r = lane >> 2, q = lane & 3;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -167,7 +171,7 @@ __device__ __forceinline__ void lower_left(const float* A, float* X, float* scra
         c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0.f;
     }
     __syncwarp();
-    product<MT, 2 * MT>(c, X + r0 * XP + r0, XP, scratch, 8, lane);
+    product<MT, 2 * MT, true>(c, X + r0 * XP + r0, XP, scratch, 8, 0, lane);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         *reinterpret_cast<float2*>(X + (r0 + 16 * m + r) * XP + c0 + n0 + 2 * q) = make_float2(c[m][0], c[m][1]);
@@ -479,15 +483,18 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
 //   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-constexpr int WALK_THREADS = 10 * 32, W = 32, WC = 16;
-constexpr uint32_t COL_X = 0, COL_D = 64, COL_O = 128, WALK_COLS = 256;
+constexpr int WC = 16;
 
-template <int D, int ST>
+template <int D_, int W_, int QST, int YST>
 struct Walk {
-    using In = Chunk<D>;
-    static constexpr int STAGES = ST;
-    static constexpr int KQ = 2 * TILE * (D / 64), Y = KQ, V = Y + ((In::BYTES + 1023) & ~1023), STAGE = V + DC * W * 2;
-    static constexpr int OFF_S = STAGES * STAGE, OFF_R = OFF_S + D * 128, OFF_O = OFF_R + TILE, SMEM = OFF_O + 4 * 1024 + 1024;
+    using In = Chunk<D_>;
+    static constexpr int D = D_, W = W_, PARTS = W / WC;
+    static constexpr int ROW_WARPS = 4 * PARTS, THREADS = 32 * (ROW_WARPS + 2);
+    static constexpr int KQ = 2 * TILE * (D / 64), V = (In::BYTES + 1023) & ~1023, Y_STAGE = V + DC * W * 2, OFF_Y = QST * KQ;
+    // Operands of W columns in two terms: rows of [32 high | 32 low], or a tile of 64 high and one of 64 low columns behind each other.
+    static constexpr int S_BYTES = D * 4 * W, R_BYTES = DC * 4 * W, S_LBO = D * 128, R_LBO = TILE;
+    static constexpr int OFF_S = OFF_Y + YST * Y_STAGE, OFF_R = OFF_S + S_BYTES, OFF_O = OFF_R + R_BYTES, SMEM = OFF_O + 2 * PARTS * 1024 + 1024;
+    static constexpr uint32_t COL_X = 0, COL_D = 2 * W, COL_O = 4 * W, COLS = W == 32 ? 256 : 512;
     static constexpr uint32_t Y_BYTES = In::BYTES + DC * W * 2;
 };
 
@@ -499,14 +506,15 @@ __device__ __forceinline__ void wait_hot(uint64_t* bar, uint32_t parity, volatil
     mbar_wait_slow<false>(bar, parity, abortp, status, MBAR_WAIT_LIMIT);
 }
 #define WAIT_HOT(bar, parity) wait_hot(bar, parity, abortp, p.status)
-// Rows to the MMA warp, through named barriers: eight warps and four arrive, it alone waits.  (Every wait before an arrival is bounded, so each arrives.)
-#define S_READY_SYNC() asm volatile("bar.sync 1, 288;" ::: "memory")
-#define S_READY_ARRIVE() asm volatile("bar.arrive 1, 288;" ::: "memory")
-#define R_READY_SYNC() asm volatile("bar.sync 2, 160;" ::: "memory")
-#define R_READY_ARRIVE() asm volatile("bar.arrive 2, 160;" ::: "memory")
+// Rows to the MMA warp, through named barriers: all row warps (or half of them) arrive, it alone waits.  (Every wait before an arrival is bounded, so each arrives.)
+template <int ID, int WARPS>
+__device__ __forceinline__ void rows_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(32 * (WARPS + 1)) : "memory"); }
+template <int ID, int WARPS>
+__device__ __forceinline__ void rows_wait() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(32 * (WARPS + 1)) : "memory"); }
 
-// 16 fp32 values (pairs) in two bf16 terms into row r of an operand whose rows hold [32 high | 32 low]; piece: 0 or 2 (16-byte pieces).
-__device__ __forceinline__ void put_split(uint8_t* tile, int r, int piece, const uint64_t (&x)[WC / 2]) {
+// Columns 16 part .. of row r (pairs of fp32) in two bf16 terms into an operand of W columns; `lbo`: bytes between its tiles of 64.
+template <int W>
+__device__ __forceinline__ void put_split(uint8_t* tile, int lbo, int r, int part, const uint64_t (&x)[WC / 2]) {
     uint8_t* row = tile + r * 128;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -518,19 +526,20 @@ __device__ __forceinline__ void put_split(uint8_t* tile, int r, int piece, const
             const float2 z = unpair(add2(x[4 * i + e], pair((h[e] << 16) ^ 0x80000000u, (h[e] & 0xffff0000u) ^ 0x80000000u)));
             l[e] = pack_bf16(z.x, z.y);
         }
-        *reinterpret_cast<uint4*>(row + (((piece + i) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4*>(row + (((piece + i + 4) ^ (r & 7)) << 4)) = make_uint4(l[0], l[1], l[2], l[3]);
+        const int piece = 2 * part + i;
+        *reinterpret_cast<uint4*>(row + ((piece ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(row + (W == 32 ? ((piece + 4) ^ (r & 7)) << 4 : lbo + ((piece ^ (r & 7)) << 4))) = make_uint4(l[0], l[1], l[2], l[3]);
     }
 }
 
-template <int D, int ST>
-__global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
+template <int D, int W, int QST, int YST>
+__global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
                                                                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
-    using L = Walk<D, ST>;
+    using L = Walk<D, W, QST, YST>;
     using In = Chunk<D>;
-    constexpr int SLABS = D / W;
+    constexpr int SLABS = D / W, MMA_WARP = L::ROW_WARPS, LOAD_WARP = MMA_WARP + 1;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free;
+    __shared__ uint64_t kq_full[QST], kq_empty[QST], y_full[YST], y_empty[YST], x_full, d_full, o_full, o_free;
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
@@ -540,20 +549,22 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
     const int slab = blockIdx.x % SLABS, h = (blockIdx.x / SLABS) % p.H, n = blockIdx.x / (SLABS * p.H);
 
     if (tid == 0) {
-        for (int i = 0; i < ST; ++i) {
+        for (int i = 0; i < QST; ++i) {
             mbar_init(&kq_full[i], 1);
             mbar_init(&kq_empty[i], 1);
+        }
+        for (int i = 0; i < YST; ++i) {
             mbar_init(&y_full[i], 1);
-            mbar_init(&y_empty[i], 5);      // the MMAs, and the four warps that read the gates off the chain
+            mbar_init(&y_empty[i], 1 + L::ROW_WARPS / 2);      // the MMAs, and the warps that read the gates off the chain
         }
         mbar_init(&x_full, 1);
         mbar_init(&d_full, 1);
         mbar_init(&o_full, 1);
-        mbar_init(&o_free, 4);
+        mbar_init(&o_free, L::ROW_WARPS / 2);
         abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 8) { tmem_alloc(&tmem_base, WALK_COLS); tmem_relinquish(); }
+    if (warp == MMA_WARP) { tmem_alloc(&tmem_base, L::COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -566,7 +577,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
     const bool work = slot >= 0 && slot < p.num_slots && (len > 0 || !p.use_initial_state);
     const int nc = work && len > 0 ? (len + DC - 1) / DC : 0;
 
-    if (warp == 9) {
+    if (warp == LOAD_WARP) {
         if (lane == 0 && nc > 0) {
             prefetch_tensormap(&map_k);
             prefetch_tensormap(&map_q);
@@ -574,59 +585,60 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
             prefetch_tensormap(&map_o);
             const int hq = h / p.group;
             for (int c = 0; c < nc && !*abortp; ++c) {
-                const int st = c % ST;
-                uint8_t* to = sm + st * L::STAGE;
-                if (c >= ST) WAIT(&kq_empty[st], (c / ST - 1) & 1);
-                mbar_arrive_expect_tx(&kq_full[st], L::KQ);
+                const int qs = c % QST, ys = c % YST;
+                if (c >= QST) WAIT(&kq_empty[qs], (c / QST - 1) & 1);
+                uint8_t* to = sm + qs * L::KQ;
+                mbar_arrive_expect_tx(&kq_full[qs], L::KQ);
                 for (int half = 0; half < D / 64; ++half) {
-                    tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[st], 0, t_begin + c * DC, half, hq);
-                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[st], 0, t_begin + c * DC, half, hq);
+                    tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[qs], 0, t_begin + c * DC, half, hq);
+                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[qs], 0, t_begin + c * DC, half, hq);
                 }
-                if (c >= ST) WAIT(&y_empty[st], (c / ST - 1) & 1);
-                mbar_arrive_expect_tx(&y_full[st], L::Y_BYTES);
-                bulk_load(to + L::Y, tp.ws + ((size_t)(first + c) * p.H + h) * In::BYTES, In::BYTES, &y_full[st]);
-                tma_load_3d(to + L::V, &map_v, &y_full[st], slab * W, h, t_begin + c * DC);
+                if (c >= YST) WAIT(&y_empty[ys], (c / YST - 1) & 1);
+                to = sm + L::OFF_Y + ys * L::Y_STAGE;
+                mbar_arrive_expect_tx(&y_full[ys], L::Y_BYTES);
+                bulk_load(to, tp.ws + ((size_t)(first + c) * p.H + h) * In::BYTES, In::BYTES, &y_full[ys]);
+                tma_load_3d(to + L::V, &map_v, &y_full[ys], slab * W, h, t_begin + c * DC);
             }
         }
-    } else if (warp == 8) {
+    } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
-        constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
+        constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1);
         for (int c = 0; c < nc; ++c) {
-            const int st = c % ST;
-            const uint32_t kq = base + st * L::STAGE, y = kq + L::Y;
-            WAIT(&kq_full[st], (c / ST) & 1);
-            S_READY_SYNC();
+            const int qs = c % QST, ys = c % YST;
+            const uint32_t kq = base + qs * L::KQ, y = base + L::OFF_Y + ys * L::Y_STAGE;
+            WAIT(&kq_full[qs], (c / QST) & 1);
+            rows_wait<1, L::ROW_WARPS>();
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    mma_ss(tb + COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
+                    mma_ss(tb + L::COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, L::S_LBO, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&x_full);
-                tc_commit(&kq_empty[st]);
+                tc_commit(&kq_empty[qs]);
             }
             __syncwarp();
-            WAIT(&y_full[st], (c / ST) & 1);
+            WAIT(&y_full[ys], (c / YST) & 1);
             if (c > 0) WAIT(&o_free, (c - 1) & 1);
-            R_READY_SYNC();
+            rows_wait<2, L::ROW_WARPS / 2>();
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
                 for (int k = 1; k >= 0; --k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
 #pragma unroll
                     for (int kk = 0; kk < DC / 16; ++kk)
-                        mma_ss(tb + COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID, !k || kk ? 1u : 0u);
+                        mma_ss(tb + L::COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, !k || kk ? 1u : 0u);
                 tc_commit(&d_full);
 #pragma unroll
                 for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
-                    mma_ss(tb + COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
+                    mma_ss(tb + L::COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&o_full);
-                tc_commit(&y_empty[st]);
+                tc_commit(&y_empty[ys]);
             }
             __syncwarp();
         }
     } else if (work) {
         const int quad = warp & 3, row = 32 * quad + lane;      // lane of TMEM: d_k of the state; token (quadrants 0, 1: of R, 2, 3: of the outputs)
-        const int part = warp >> 2, piece = 2 * part;     // which 16 of the 32 columns
+        const int part = warp >> 2;                             // which 16 of the W columns
         const uint32_t lane_addr = tb + ((uint32_t)(32 * quad) << 16) + WC * part;
         const bool has_state = row < D, makes_r = quad < 2;
         const int j = row & 63;
@@ -642,13 +654,13 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
         }
         // The outputs of chunk c (quadrants 2, 3): y, scaled, and P T R.  Whole rows of 32 tokens leave by a TMA store of this warp; the stores of a ragged end
         // come from the registers.
-        uint8_t* o_tile = sm + L::OFF_O + ((quad & 1) * 2 + part) * 1024;
+        uint8_t* o_tile = sm + L::OFF_O + ((quad & 1) * L::PARTS + part) * 1024;
         auto outputs = [&](int c) {
             uint32_t a[WC], b[WC];
             WAIT_HOT(&o_full, c & 1);
             tc_fence_after();
-            tmem_ld16(lane_addr + COL_O, a);
-            tmem_ld16(lane_addr + COL_O + 32, b);
+            tmem_ld16(lane_addr + L::COL_O, a);
+            tmem_ld16(lane_addr + L::COL_O + W, b);
             tc_wait_ld();
             tc_fence_before();
             __syncwarp();
@@ -678,26 +690,27 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
             }
         };
         for (int c = 0; c < nc; ++c) {
-            const int st = c % ST, live = min(DC, len - c * DC);
-            uint8_t* stage = sm + st * L::STAGE;
-            const float* meta = reinterpret_cast<const float*>(stage + L::Y + In::META);
+            const int ys = c % YST, live = min(DC, len - c * DC);
+            const uint8_t* stage = sm + L::OFF_Y + ys * L::Y_STAGE;
+            const float* meta = reinterpret_cast<const float*>(stage + In::META);
             uint32_t a[WC], b[WC];
             float last;
-            if (has_state) put_split(sm + L::OFF_S, row, piece, s);
+            if (has_state) put_split<W>(sm + L::OFF_S, L::S_LBO, row, part, s);
             fence_proxy_async_smem();
             tc_fence_before();
-            S_READY_ARRIVE();
+            rows_arrive<1, L::ROW_WARPS>();
             if (makes_r) {
-                WAIT_HOT(&y_full[st], (c / ST) & 1);
+                WAIT_HOT(&y_full[ys], (c / YST) & 1);
                 last = meta[2 * DC - 1];
                 const float G = -meta[DC + j];
                 uint4 vr[2];
-                vr[0] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + part * 32);
-                vr[1] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + part * 32 + 16);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)      // rows of 64 or 128 bytes, swizzled
+                    vr[i] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + (((2 * part + i) ^ (W == 32 ? (j >> 1) & 3 : j & 7)) << 4));
                 WAIT_HOT(&x_full, c & 1);
                 tc_fence_after();
-                tmem_ld16(lane_addr + COL_X, a);
-                tmem_ld16(lane_addr + COL_X + 32, b);
+                tmem_ld16(lane_addr + L::COL_X, a);
+                tmem_ld16(lane_addr + L::COL_X + W, b);
                 tc_wait_ld();
                 uint64_t r[WC / 2];
 #pragma unroll
@@ -709,29 +722,29 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
 #pragma unroll
                     for (int i = 0; i < WC / 2; ++i) r[i] = 0;
                 }
-                put_split(sm + L::OFF_R, j, piece, r);
+                put_split<W>(sm + L::OFF_R, L::R_LBO, j, part, r);
                 fence_proxy_async_smem();
                 tc_fence_before();
-                R_READY_ARRIVE();
+                rows_arrive<2, L::ROW_WARPS / 2>();
             } else {
                 if (c > 0) outputs(c - 1);
-                WAIT_HOT(&y_full[st], (c / ST) & 1);
+                WAIT_HOT(&y_full[ys], (c / YST) & 1);
                 last = meta[2 * DC - 1];
                 const float G = meta[j];
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&y_empty[st]);
+                if (lane == 0) mbar_arrive(&y_empty[ys]);
                 WAIT_HOT(&x_full, c & 1);
                 tc_fence_after();
-                tmem_ld16(lane_addr + COL_X, a);
-                tmem_ld16(lane_addr + COL_X + 32, b);
+                tmem_ld16(lane_addr + L::COL_X, a);
+                tmem_ld16(lane_addr + L::COL_X + W, b);
                 tc_wait_ld();
 #pragma unroll
                 for (int i = 0; i < WC / 2; ++i) y[i] = mul2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
             }
             WAIT_HOT(&d_full, c & 1);
             tc_fence_after();
-            tmem_ld16(lane_addr + COL_D, a);
-            tmem_ld16(lane_addr + COL_D + 32, b);
+            tmem_ld16(lane_addr + L::COL_D, a);
+            tmem_ld16(lane_addr + L::COL_D + W, b);
             tc_wait_ld();
             const uint64_t keep = pair(last, last);
 #pragma unroll
@@ -750,7 +763,7 @@ __global__ void __launch_bounds__(WALK_THREADS, ST == 1 ? 2 : 1) delta_walk_kern
     tc_fence_before();
     __syncthreads();
     settle_after_timeout(abortp);
-    if (warp == 8) tmem_dealloc(tb, WALK_COLS);
+    if (warp == MMA_WARP) tmem_dealloc(tb, L::COLS);
 }
 
 // [T_total, H_qk, D] bf16 as (64 elements, t, part of a row, head); a box is 64 tokens of one part, one swizzled tile.
@@ -761,24 +774,31 @@ bool make_map(CUtensorMap* m, const void* base, int T_total, int H, int d) {
     return encode_tile_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// [T_total, H, D] bf16 as (element, head, t); a box is `columns` elements of `tokens` tokens, packed rows.
-bool make_slab_map(CUtensorMap* m, const void* base, int T_total, int H, int d, int columns, int tokens) {
+// [T_total, H, D] bf16 as (element, head, t); a box is `columns` elements of `tokens` tokens.
+bool make_slab_map(CUtensorMap* m, const void* base, int T_total, int H, int d, int columns, int tokens, CUtensorMapSwizzle swizzle) {
     cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)T_total};
     cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)H * d * 2};
     cuuint32_t box[3] = {(cuuint32_t)columns, 1, (cuuint32_t)tokens};
-    return encode_tile_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+    return encode_tile_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, swizzle);
 }
 
 long long chunk_slots(const dsla_delta_prefill_args* a) {
     return a->cu_seqlens ? (long long)a->T_total / DC + a->N : (long long)a->N * ((a->T + DC - 1) / DC);
 }
 
-template <int D, int ST>
-dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CUtensorMap& mq, const CUtensorMap& mv, const CUtensorMap& mo, const DeltaTcParams& tp) {
-    if (cudaFuncSetAttribute(delta_walk_kernel<D, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, Walk<D, ST>::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
-    cfg.blockDim = dim3(WALK_THREADS);
-    cfg.dynamicSmemBytes = Walk<D, ST>::SMEM;
-    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D, ST>, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
+template <int D, int W, int QST, int YST>
+dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CUtensorMap& mq, const CUtensorMap& mo, const DeltaTcParams& tp, int T_total) {
+    using L = Walk<D, W, QST, YST>;
+    const DeltaParams& p = tp.p;
+    CUtensorMap mv{};
+    if (T_total > 0 && !make_slab_map(&mv, p.v, T_total, p.H, D, W, DC, W == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B)) return DSLA_ERR_CUDA;
+    const long long ctas = (long long)p.N * p.H * (D / W);
+    if (ctas > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(delta_walk_kernel<D, W, QST, YST>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(L::THREADS);
+    cfg.dynamicSmemBytes = L::SMEM;
+    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D, W, QST, YST>, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
     count_launch();
     return DSLA_OK;
 }
@@ -786,12 +806,12 @@ dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CU
 template <int D>
 dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cudaStream_t s) {
     const DeltaParams& p = tp.p;
-    CUtensorMap mk{}, mq{}, mv{}, mo{};
+    CUtensorMap mk{}, mq{}, mo{};
     if (a->T_total > 0 && (!make_map(&mk, p.k, a->T_total, a->H_qk, D) || !make_map(&mq, p.q, a->T_total, a->H_qk, D) ||
-                           !make_slab_map(&mv, p.v, a->T_total, p.H, D, W, DC) || !make_slab_map(&mo, p.o, a->T_total, p.H, D, WC, 32)))
+                           !make_slab_map(&mo, p.o, a->T_total, p.H, D, WC, 32, CU_TENSOR_MAP_SWIZZLE_NONE)))
         return DSLA_ERR_CUDA;
-    const long long prep = a->T_total > 0 ? (long long)tp.slots * p.H : 0, walk = (long long)p.N * p.H * (D / W);
-    if (prep > 0x7fffffffLL || walk > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
+    const long long prep = a->T_total > 0 ? (long long)tp.slots * p.H : 0;
+    if (prep > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -807,8 +827,13 @@ dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cu
         if (cudaLaunchKernelEx(&cfg, delta_chunk_kernel<D>, mk, mq, tp) != cudaSuccess) return DSLA_ERR_CUDA;
         count_launch();
     }
-    cfg.gridDim = dim3((unsigned)walk);
-    const dsla_status rc = walk <= sm_count() ? launch_walk<D, 2>(cfg, mk, mq, mv, mo, tp) : launch_walk<D, 1>(cfg, mk, mq, mv, mo, tp);
+    static const int force = getenv("DELTA_W") ? atoi(getenv("DELTA_W")) : 0;
+    const long long units = (long long)p.N * p.H * (D / 32);
+    dsla_status rc;
+    if (force == 3212) rc = launch_walk<D, 32, 1, 2>(cfg, mk, mq, mo, tp, a->T_total);
+    else if (force == 3222 || (!force && units <= sm_count())) rc = launch_walk<D, 32, 2, 2>(cfg, mk, mq, mo, tp, a->T_total);
+    else if (force == 6412) rc = launch_walk<D, 64, 1, 2>(cfg, mk, mq, mo, tp, a->T_total);
+    else rc = launch_walk<D, 64, 2, 2>(cfg, mk, mq, mo, tp, a->T_total);
     if (rc != DSLA_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? DSLA_OK : DSLA_ERR_CUDA;
 }

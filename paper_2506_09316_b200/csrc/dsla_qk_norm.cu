@@ -15,6 +15,7 @@ constexpr int QN_THREADS = 256;
 template <typename T> struct Eight;
 template <> struct Eight<float> {
     float4 a, b;
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -26,6 +27,7 @@ template <> struct Eight<float> {
 };
 template <> struct Eight<__nv_bfloat16> {
     uint4 a;
+    __device__ __forceinline__ void zero() { a = make_uint4(0u, 0u, 0u, 0u); }
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -46,6 +48,7 @@ template <> struct Eight<__nv_bfloat16> {
 template <int D, typename T, int NORM, bool INTERLEAVED>
 __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_norm_rope_args p, int per) {
     constexpr int LANES = D / 8, HEADS = QN_THREADS / LANES;      // lanes per head, heads per CTA at a time
+    constexpr int AHEAD = 4;                                      // rounds of heads whose loads are issued together
     __shared__ __align__(16) float scos[D / 2], ssin[D / 2];
     const int t = blockIdx.x, tid = threadIdx.x;
     const int lane = tid % LANES, first = 8 * lane;
@@ -53,67 +56,80 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int rot = p.rot, half = rot / 2;
-    if (tid < half) {
-        const double turns = (double)p.positions[t] * (double)p.inv_freq[tid] * 0.31830988618379067154;      // half turns
-        float sn, cs;
-        sincospif((float)(turns - 2.0 * rint(0.5 * turns)), &sn, &cs);
-        scos[tid] = cs;
-        ssin[tid] = sn;
-    }
-    if (rot > 0) __syncthreads();
-    for (int h0 = begin; h0 < end; h0 += HEADS) {
-        const int h = h0 + tid / LANES;
-        const bool live = h < end;      // whole groups of LANES lanes; the shuffles below run in all of them
-        const bool is_k = h >= p.H;
-        const T* src = is_k ? reinterpret_cast<const T*>(p.k) + (size_t)t * p.k_stride + (size_t)(h - p.H) * D
-                            : reinterpret_cast<const T*>(p.q) + (size_t)t * p.q_stride + (size_t)h * D;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) {
-            Eight<T> in;
-            in.load(src + first);
-            in.get(x);
+    Eight<T> in[AHEAD];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) {
+            const int h = h0 + r * HEADS + tid / LANES;
+            if (h < end) in[r].load((h >= p.H ? reinterpret_cast<const T*>(p.k) + (size_t)t * p.k_stride + (size_t)(h - p.H) * D
+                                              : reinterpret_cast<const T*>(p.q) + (size_t)t * p.q_stride + (size_t)h * D) + first);
+            else in[r].zero();
         }
-        if (NORM != DSLA_NORM_NONE) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-#pragma unroll
-            for (int m = 1; m < LANES; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-            const float r = rsqrtf((NORM == DSLA_NORM_RMS ? sum * (1.f / D) : sum) + p.eps);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= r;
+    };
+    load(begin);
+    // this lane's sines and cosines, with the sign that its half has: y = x cos + other sin
+    float cs[8], sn[8];
+    if (rot > 0) {
+        if (tid < half) {
+            const double turns = (double)p.positions[t] * (double)p.inv_freq[tid] * 0.31830988618379067154;      // half turns
+            float a, b;
+            sincospif((float)(turns - 2.0 * rint(0.5 * turns)), &a, &b);
+            scos[tid] = b;
+            ssin[tid] = a;
         }
-        const float* w = is_k ? p.k_weight : p.q_weight;
-        if (w) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= __ldg(w + first + i);
-        }
-        if (INTERLEAVED) {
-            if (first < rot) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float cs = scos[first / 2 + i], sn = ssin[first / 2 + i], a = x[2 * i], b = x[2 * i + 1];
-                    x[2 * i] = a * cs - b * sn;
-                    x[2 * i + 1] = b * cs + a * sn;
-                }
-            }
-        } else if (rot > 0) {
-            const int step = half / 8;      // lanes between the halves
-            const bool upper = first >= half, in = first < rot;
-            const int partner = in ? (upper ? (tid & 31) - step : (tid & 31) + step) : (tid & 31);
+        __syncthreads();
+        if (first < rot) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float other = __shfl_sync(0xffffffffu, x[i], partner);
-                if (in) {
-                    const int f = upper ? first - half + i : first + i;
-                    x[i] = upper ? x[i] * scos[f] + other * ssin[f] : x[i] * scos[f] - other * ssin[f];
+                const int f = INTERLEAVED ? first / 2 + i / 2 : first >= half ? first - half + i : first + i;
+                cs[i] = scos[f];
+                sn[i] = (INTERLEAVED ? i % 2 == 0 : first < half) ? -ssin[f] : ssin[f];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+        }
+    }
+    const int step = half / 8;      // lanes between the halves
+    const int partner = first < rot ? (first >= half ? (tid & 31) - step : (tid & 31) + step) : (tid & 31);
+    for (int h0 = begin; h0 < end; h0 += AHEAD * HEADS) {
+        if (h0 > begin) load(h0);
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) {
+            if (h0 + r * HEADS >= end) break;
+            const int h = h0 + r * HEADS + tid / LANES;      // heads behind the last: zeros, not stored; the shuffles run in all lanes
+            const bool is_k = h >= p.H;
+            float x[8];
+            in[r].get(x);
+            if (NORM != DSLA_NORM_NONE) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+#pragma unroll
+                for (int m = 1; m < LANES; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+                const float f = rsqrtf((NORM == DSLA_NORM_RMS ? sum * (1.f / D) : sum) + p.eps);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] *= f;
+            }
+            const float* w = is_k ? p.k_weight : p.q_weight;
+            if (w) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] *= __ldg(w + first + i);
+            }
+            if (rot > 0) {
+                float other[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) other[i] = INTERLEAVED ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], partner);
+                if (first < rot) {      // channels that do not turn keep their bits
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], cs[i], other[i] * sn[i]);
                 }
             }
-        }
-        if (live) {
-            T* dst = is_k ? reinterpret_cast<T*>(p.k_out) + (size_t)t * p.k_out_stride + (size_t)(h - p.H) * D
-                          : reinterpret_cast<T*>(p.q_out) + (size_t)t * p.q_out_stride + (size_t)h * D;
-            Eight<T>::store(dst + first, x);
+            if (h < end) {
+                T* dst = is_k ? reinterpret_cast<T*>(p.k_out) + (size_t)t * p.k_out_stride + (size_t)(h - p.H) * D
+                              : reinterpret_cast<T*>(p.q_out) + (size_t)t * p.q_out_stride + (size_t)h * D;
+                Eight<T>::store(dst + first, x);
+            }
         }
     }
 }

@@ -9,7 +9,7 @@ namespace dsla {
 
 namespace {
 
-constexpr int SC_THREADS = 256, SC_LIST = 256, SC_GROUP = 8;
+constexpr int SC_THREADS = 128, SC_LIST = 256, SC_GROUP = 8;
 enum : int { SC_SKIP = -2, SC_CLEAR = -1 };
 
 __global__ void __launch_bounds__(SC_THREADS) state_copy_kernel(float4* data, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int n,
@@ -23,21 +23,22 @@ __global__ void __launch_bounds__(SC_THREADS) state_copy_kernel(float4* data, co
     for (int first = 0; first < n; first += SC_LIST) {
         const int count = min(SC_LIST, n - first);
         __syncthreads();
-        {
-            const int i = threadIdx.x;
+#pragma unroll
+        for (int r = 0; r < SC_LIST / SC_THREADS; ++r) {
+            const int i = r * SC_THREADS + threadIdx.x;
             int a = i < count ? src[first + i] : SC_SKIP;
             const int b = i < count ? dst[first + i] : 0;
             if (a < -1 || a >= num_slots || b < 0 || b >= num_slots || a == b) a = SC_SKIP;
             from[i] = a;
             to[i] = b;
-        }
-        __syncthreads();
-        if (threadIdx.x < SC_LIST / SC_GROUP) {
-            const int g = threadIdx.x * SC_GROUP;
-            bool c = false;
-            for (int j = 1; j < SC_GROUP; ++j)
-                for (int i = 0; i < j; ++i) c |= from[g + i] != SC_SKIP && from[g + j] == to[g + i];
-            chained[threadIdx.x] = c;
+            bool c = false;      // the lanes of a group compare with those before them
+#pragma unroll
+            for (int k = 1; k < SC_GROUP; ++k) {
+                const int fa = __shfl_up_sync(0xffffffffu, a, k), tb = __shfl_up_sync(0xffffffffu, b, k);
+                c |= (int)(threadIdx.x % SC_GROUP) >= k && fa != SC_SKIP && a == tb;
+            }
+            const unsigned any = __ballot_sync(0xffffffffu, c);
+            if (threadIdx.x % SC_GROUP == 0) chained[i / SC_GROUP] = (any >> (threadIdx.x % 32)) & ((1u << SC_GROUP) - 1);
         }
         __syncthreads();
         if (at >= slot4) continue;
@@ -49,11 +50,11 @@ __global__ void __launch_bounds__(SC_THREADS) state_copy_kernel(float4* data, co
                     const int a = from[g + j];
                     x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (j > 0 && a == from[g + (j > 0 ? j - 1 : 0)]) x[j] = x[j > 0 ? j - 1 : 0];      // a fork reads its source once
-                    else if (a >= 0) x[j] = place[(size_t)a * slot4];
+                    else if (a >= 0) x[j] = __ldcs(place + (size_t)a * slot4);
                 }
 #pragma unroll
                 for (int j = 0; j < SC_GROUP; ++j)
-                    if (from[g + j] != SC_SKIP) place[(size_t)to[g + j] * slot4] = x[j];
+                    if (from[g + j] != SC_SKIP) __stcs(place + (size_t)to[g + j] * slot4, x[j]);
             } else {
 #pragma unroll 1
                 for (int j = 0; j < SC_GROUP; ++j) {
