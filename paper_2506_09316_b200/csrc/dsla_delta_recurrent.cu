@@ -1,8 +1,8 @@
-// Gated delta rule over prompts, token by token on CUDA cores in fp32.  With S' the state before token t - 1,
-//     y = k_t S = g_{t-1} (k_t S') + (k_t.k_{t-1}) u_{t-1},     z = q_t S = g_{t-1} (q_t S') + (q_t.k_{t-1}) u_{t-1},
-//     u_t = beta_t (v_t - g_t y),     o_t = scale (g_t z + (q_t.k_t) u_t),     S <- g_t S + k_t^T u_t :
-// the sums over d_k that token t needs are taken from the state one token earlier, so they run while token t - 1 is still being finished, and only
-// two products lie between one u and the next.  (Sums from the state itself, four threads to a column: 112 us for 512 tokens of 4 heads of 64.)
+// Gated delta rule over prompts, token by token on CUDA cores in fp32.  With S" the state before token t - 2,
+//     k_t S = g_{t-1} (g_{t-2} (k_t S") + (k_t.k_{t-2}) u_{t-2}) + (k_t.k_{t-1}) u_{t-1}     and the same with q_t,
+//     u_t = beta_t (v_t - g_t k_t S),     o_t = scale (g_t q_t S + (q_t.k_t) u_t),     S <- g_t S + k_t^T u_t :
+// the sums over d_k that token t needs are taken from the state two tokens earlier, so their reduction runs while the tokens before t are being finished, and
+// only two products lie between one u and the next.  (512 tokens of 4 heads of 64: sums from the state itself 112 us, from one token earlier 65 us.)
 // A CTA owns (sequence, head, 16 columns of d_v); eight threads share a column, each with D / 8 rows of it in registers.  Tokens are staged in blocks as fp32,
 // three blocks deep in shared memory, and one more on its way in registers; behind a sequence's end they are tokens without keys, which change
 // nothing.  Bound by that chain: it serves fp32 (whose products the tensor cores do not take) and whoever asks for it; bf16 prompts have the
@@ -56,7 +56,8 @@ __global__ void __launch_bounds__(DR_THREADS) delta_recurrent_kernel(const Delta
     constexpr int LOADS = BLOCK * D / 4 / DR_THREADS;      // 16-byte pieces of q, and of k, per thread and block
     __shared__ __align__(16) float sq[3][BLOCK][D], sk[3][BLOCK][D];
     __shared__ float sv[3][BLOCK][DR_COLS], sg[3][BLOCK], sb[3][BLOCK];
-    __shared__ float skk[3][BLOCK], sqk1[3][BLOCK], sqk[3][BLOCK];      // k_t.k_{t-1}, q_t.k_{t-1}, q_t.k_t
+    __shared__ float4 sc[3][BLOCK];                                         // k_t.k_{t-1}, k_t.k_{t-2}, q_t.k_{t-1}, q_t.k_{t-2}
+    __shared__ float sqk[3][BLOCK];                                         // q_t.k_t
     const int tid = threadIdx.x, lane = tid & 31;
     const int slab = blockIdx.x % SLABS;
     const int h = (blockIdx.x / SLABS) % p.H;
@@ -124,34 +125,34 @@ __global__ void __launch_bounds__(DR_THREADS) delta_recurrent_kernel(const Delta
     };
     auto dots = [&](int blk) {       // products of a block's keys and queries with each other; 128 / BLOCK threads to a token
         constexpr int PER = DR_THREADS / BLOCK;
-        const int buf = blk % 3, t = tid / PER;
-        const float* before = t > 0 ? sk[buf][t - 1] : sk[(blk + 2) % 3][BLOCK - 1];
-        float a = 0.f, b = 0.f, d = 0.f;
+        const int buf = blk % 3, t = tid / PER, before = (blk + 2) % 3;
+        const float* one = t > 0 ? sk[buf][t - 1] : sk[before][BLOCK - 1];
+        const float* two = t > 1 ? sk[buf][t - 2] : sk[before][BLOCK - 2 + t];
+        float x[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < D / (4 * PER); ++i) {
             const int at = 4 * (i * PER + tid % PER);
             const float4 k = *reinterpret_cast<const float4*>(&sk[buf][t][at]), q = *reinterpret_cast<const float4*>(&sq[buf][t][at]);
-            const float4 o = *reinterpret_cast<const float4*>(before + at);
-            a += k.x * o.x + k.y * o.y + k.z * o.z + k.w * o.w;
-            b += q.x * o.x + q.y * o.y + q.z * o.z + q.w * o.w;
-            d += q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
+            const float4 a = *reinterpret_cast<const float4*>(one + at), b = *reinterpret_cast<const float4*>(two + at);
+            x[0] += k.x * a.x + k.y * a.y + k.z * a.z + k.w * a.w;
+            x[1] += k.x * b.x + k.y * b.y + k.z * b.z + k.w * b.w;
+            x[2] += q.x * a.x + q.y * a.y + q.z * a.z + q.w * a.w;
+            x[3] += q.x * b.x + q.y * b.y + q.z * b.z + q.w * b.w;
+            x[4] += q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
         }
 #pragma unroll
-        for (int m = 1; m < PER; m <<= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, m);
-            b += __shfl_xor_sync(0xffffffffu, b, m);
-            d += __shfl_xor_sync(0xffffffffu, d, m);
-        }
+        for (int m = 1; m < PER; m <<= 1)
+#pragma unroll
+            for (int i = 0; i < 5; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], m);
         if (tid % PER == 0) {
-            const bool first = blk == 0 && t == 0;      // no token before it
-            skk[buf][t] = first ? 0.f : a;
-            sqk1[buf][t] = first ? 0.f : b;
-            sqk[buf][t] = d;
+            sc[buf][t] = make_float4(x[0], x[1], x[2], x[3]);
+            sqk[buf][t] = x[4];
         }
     };
     const int blocks = (len + BLOCK - 1) / BLOCK;
-    float u = 0.f, g = 1.f, ya = 0.f, za = 0.f;      // of the token before: u, gate; of this one: k and q times the state before that token
-    const float* kp = sk[2][BLOCK - 1];               // the key of the token before
+    float u1 = 0.f, g1 = 1.f, u2 = 0.f, g2 = 1.f;      // of the two tokens before this one
+    float ya = 0.f, za = 0.f, py = 0.f, pz = 0.f;      // this token's sums; this thread's part of the next one's
+    const float* kp = sk[2][BLOCK - 1];                 // the key of the token before
     auto sums = [&](const float* k, const float* q) {
         uint64_t y0 = 0, y1 = 0, z0 = 0, z1 = 0;
 #pragma unroll
@@ -160,11 +161,11 @@ __global__ void __launch_bounds__(DR_THREADS) delta_recurrent_kernel(const Delta
             y0 = fma2(kk.x, s[2 * i], y0); y1 = fma2(kk.y, s[2 * i + 1], y1);
             z0 = fma2(qq.x, s[2 * i], z0); z1 = fma2(qq.y, s[2 * i + 1], z1);
         }
-        ya = over_parts(sum2(y0, y1));
-        za = over_parts(sum2(z0, z1));
+        py = sum2(y0, y1);
+        pz = sum2(z0, z1);
     };
     auto advance = [&]() {           // the state takes in the token before
-        const uint64_t gg = pair(g, g), uu = pair(u, u);
+        const uint64_t gg = pair(g1, g1), uu = pair(u1, u1);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(kp + 32 * i + 4 * part);
@@ -177,12 +178,15 @@ __global__ void __launch_bounds__(DR_THREADS) delta_recurrent_kernel(const Delta
         put(0);
         fetch(1);
         put(1);
-        if (tid < D) sk[2][BLOCK - 1][tid] = 0.f;
+        for (int i = tid; i < 2 * D; i += DR_THREADS) sk[2][BLOCK - 2 + i / D][i % D] = 0.f;      // no tokens before the first
         __syncthreads();
         dots(0);
         dots(1);
         fetch(2);
         sums(sk[0][0], sq[0][0]);
+        ya = over_parts(py);
+        za = over_parts(pz);
+        sums(sk[0][1], sq[0][1]);
         __syncthreads();
     }
     T* o = reinterpret_cast<T*>(p.o) + ((size_t)t_begin * p.H + h) * D + col;
@@ -191,19 +195,31 @@ __global__ void __launch_bounds__(DR_THREADS) delta_recurrent_kernel(const Delta
         const int buf = blk % 3, next = (blk + 1) % 3, left = len - blk * BLOCK;
 #pragma unroll
         for (int t = 0; t < BLOCK; ++t) {
+            const float4 c4 = sc[buf][t];
             const float gt = sg[buf][t], bt = sb[buf][t];
-            const float y = fmaf(skk[buf][t], u, g * ya), z = fmaf(sqk1[buf][t], u, g * za);
+            const float yb = g1 * fmaf(c4.y, u2, g2 * ya), zb = g1 * fmaf(c4.w, u2, g2 * za);
+            // the next token's sums close, the state takes in the token before, the sums of the token after next begin
+            float cy = py, cz = pz;
+            cy += __shfl_xor_sync(0xffffffffu, cy, 4);
+            cz += __shfl_xor_sync(0xffffffffu, cz, 4);
             advance();
-            kp = sk[buf][t];
-            if (t + 1 < BLOCK) sums(sk[buf][t + 1], sq[buf][t + 1]);
-            else sums(sk[next][0], sq[next][0]);
-            u = bt * fmaf(-gt, y, sv[buf][t][c]);
-            g = gt;
+            cy += __shfl_xor_sync(0xffffffffu, cy, 8);
+            cz += __shfl_xor_sync(0xffffffffu, cz, 8);
+            if (t + 2 < BLOCK) sums(sk[buf][t + 2], sq[buf][t + 2]);
+            else sums(sk[next][t + 2 - BLOCK], sq[next][t + 2 - BLOCK]);
+            cy += __shfl_xor_sync(0xffffffffu, cy, 16);
+            cz += __shfl_xor_sync(0xffffffffu, cz, 16);
+            const float u = bt * fmaf(-gt, fmaf(c4.x, u1, yb), sv[buf][t][c]), z = fmaf(c4.z, u1, zb);
             if (part == 0 && t < left) o[(size_t)t * step] = from_f32<T>(fmaf(sqk[buf][t], u, gt * z));
+            ya = cy;
+            za = cz;
+            u2 = u1; g2 = g1;
+            u1 = u; g1 = gt;
+            kp = sk[buf][t];
         }
         o += (size_t)BLOCK * step;
         __syncthreads();
-        if (blk + 2 < blocks + 1) {      // (the last block still looks one token ahead)
+        if (blk + 1 < blocks) {      // (the last block still looks two tokens ahead)
             put(blk + 2);
             fetch(blk + 3);
             __syncthreads();

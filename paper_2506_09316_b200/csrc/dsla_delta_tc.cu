@@ -11,7 +11,6 @@
 // Y is made of), with fp32 sums; (I + A)^-1 is fp32.  The state itself stays in fp32 registers and each chunk adds one tensor-core sum to
 // it, with rounding.  P T, which reaches only the bf16 output, has one term.
 #include <cuda.h>
-#include <cstdlib>
 
 #include "dsla_internal.cuh"
 #include "tc_utils.cuh"
@@ -133,50 +132,32 @@ __device__ __forceinline__ void tf32_terms(float x, uint32_t& hi, uint32_t& lo) 
     hi = __float_as_uint(x) & 0xffffe000u;
     lo = __float_as_uint(x - __uint_as_float(hi));
 }
-// c[m tile] += M[16 MT x 8 KT] B[8 KT x 8], both in shared memory (row pitches pa, pb), as products of two TF32 terms.
-// Steps of 8 before k_first meet zeros of B; with LOWER, M is lower triangular.
-template <int MT, int KT, bool LOWER>
-__device__ __forceinline__ void product(float (&c)[MT][4], const float* M, int pa, const float* B, int pb, int k_first, int lane) {
+// 16 rows of M[16 x 8 KT] B[8 KT x 8], both in shared memory (row pitches pa, pb), as products of two TF32 terms; steps of 8 from k_first up to k_last - 1.
+template <int KT>
+__device__ __forceinline__ void product(float (&c)[4], const float* M, int pa, const float* B, int pb, int k_first, int k_last, int lane) {
     const int r = lane >> 2, q = lane & 3;
+    float c1[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};      // (three sums side by side: an MMA waits 35 cycles for the one before it)
+    c[0] = c[1] = c[2] = c[3] = 0.f;
 #pragma unroll
     for (int k = 0; k < KT; ++k) {
-        if (k < k_first) continue;
-        uint32_t bh[2], bl[2];
+        if (k < k_first || k >= k_last) continue;
+        uint32_t ah[4], al[4], bh[2], bl[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) tf32_terms(B[(8 * k + q + 4 * i) * pb + r], bh[i], bl[i]);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (LOWER && 2 * m + 1 < k) continue;
-            uint32_t ah[4], al[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tf32_terms(M[(16 * m + r + 8 * (i & 1)) * pa + 8 * k + q + 4 * (i >> 1)], ah[i], al[i]);
-            mma_tf32(c[m], al, bh);
-            mma_tf32(c[m], ah, bl);
-            mma_tf32(c[m], ah, bh);
-        }
+        for (int i = 0; i < 4; ++i) tf32_terms(M[(r + 8 * (i & 1)) * pa + 8 * k + q + 4 * (i >> 1)], ah[i], al[i]);
+        mma_tf32(c1, al, bh);
+        mma_tf32(c2, ah, bl);
+        mma_tf32(c, ah, bh);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] += c1[i] + c2[i];
 }
-// Columns n0 .. n0 + 7 of the lower left block of the inverse: rows r0 .., columns c0 .., blocks of 16 MT.
-template <int MT>
-__device__ __forceinline__ void lower_left(const float* A, float* X, float* scratch, int r0, int c0, int n0, int lane) {
-    float c[MT][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0.f;
-    product<MT, 2 * MT, false>(c, A + r0 * XP + c0, XP, X + c0 * XP + c0 + n0, XP, n0 / 8, lane);
+// A 16 x 8 fragment to rows r0 .. of a matrix of pitch `pitch`, scaled.
+__device__ __forceinline__ void put_fragment(float* M, int pitch, const float (&c)[4], float f, int lane) {
     const int r = lane >> 2, q = lane & 3;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        *reinterpret_cast<float2*>(scratch + (16 * m + r) * 8 + 2 * q) = make_float2(-c[m][0], -c[m][1]);
-        *reinterpret_cast<float2*>(scratch + (16 * m + r + 8) * 8 + 2 * q) = make_float2(-c[m][2], -c[m][3]);
-        c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0.f;
-    }
-    __syncwarp();
-    product<MT, 2 * MT, true>(c, X + r0 * XP + r0, XP, scratch, 8, 0, lane);
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        *reinterpret_cast<float2*>(X + (r0 + 16 * m + r) * XP + c0 + n0 + 2 * q) = make_float2(c[m][0], c[m][1]);
-        *reinterpret_cast<float2*>(X + (r0 + 16 * m + r + 8) * XP + c0 + n0 + 2 * q) = make_float2(c[m][2], c[m][3]);
-    }
+    *reinterpret_cast<float2*>(M + r * pitch + 2 * q) = make_float2(f * c[0], f * c[1]);
+    *reinterpret_cast<float2*>(M + (r + 8) * pitch + 2 * q) = make_float2(f * c[2], f * c[3]);
 }
 
 template <int D>
@@ -193,10 +174,11 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
     const DeltaParams& p = tp.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abortp = &abort_flag;
-    const int h = blockIdx.x % p.H, at = blockIdx.x / p.H;
+    const int h = blockIdx.x % p.H;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int n, t_begin, len, first;
+    const int at = blockIdx.x / p.H;
     if (p.cu_seqlens) {      // the last sequence whose slots begin at or before this one
         int lo = 0, hi = p.N - 1;
         while (lo < hi) {
@@ -212,6 +194,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
     const int c = at - first;
     if (c < 0 || c * DC >= len) return;
     const int live = min(DC, len - c * DC), t0 = t_begin + c * DC;
+    const int ahead = (c + 1 + 448 / p.H) * DC;
 
     if (tid == 0) {
         mbar_init(&full, 1);
@@ -224,6 +207,11 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
             tma_load_4d(sm + half * 2 * TILE, &map_k, &full, 0, t0, half, hq);
             tma_load_4d(sm + half * 2 * TILE + TILE, &map_q, &full, 0, t0, half, hq);
         }
+        if (ahead < len)      // what a CTA some 450 from here will load
+            for (int half = 0; half < D / 64; ++half) {
+                tma_prefetch_4d(&map_k, 0, t_begin + ahead, half, hq);
+                tma_prefetch_4d(&map_q, 0, t_begin + ahead, half, hq);
+            }
     }
     if (warp == 1) { tmem_alloc(&tmem_base, 128); tmem_relinquish(); }
     if (warp == 2) {
@@ -238,6 +226,11 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
             x = log2f(x < 0.f ? 0.f : x);
             run[i] = x < -300.f ? -300.f : x;      // a gate of 0: products that contain it are an exact zero
             beta[i] = j < live ? p.beta[g] : 0.f;
+            if (ahead + j < len) {
+                const size_t far = (size_t)(t_begin + ahead + j) * p.H + h;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(p.gate + far));
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(p.beta + far));
+            }
         }
         run[1] += run[0];
         double total = run[1];
@@ -370,10 +363,26 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
             *reinterpret_cast<float4*>(X + (32 * k + (i >> 2)) * XP + 32 * k + 16 + 4 * (i & 3)) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncthreads();
-    float* scratch = reinterpret_cast<float*>(work + PREP_SCRATCH) + (warp & 3) * 256;
-    if (warp < 4) lower_left<1>(A, X, scratch, 32 * (warp >> 1) + 16, 32 * (warp >> 1), 8 * (warp & 1), lane);
+    float* scratch = reinterpret_cast<float*>(work + PREP_SCRATCH) + (warp & 3) * 256;      // [rows][8] of this warp's, or this pair's, columns
+    if (warp < 4) {      // pairs of blocks of 16: warp = pair and 8 columns
+        const int r0 = 32 * (warp >> 1) + 16, c0 = r0 - 16, n0 = 8 * (warp & 1);
+        float f[4];
+        product<2>(f, A + r0 * XP + c0, XP, X + c0 * XP + c0 + n0, XP, n0 / 8, 2, lane);
+        put_fragment(scratch, 8, f, -1.f, lane);
+        __syncwarp();
+        product<2>(f, X + r0 * XP + r0, XP, scratch, 8, 0, 2, lane);
+        put_fragment(X + r0 * XP + c0 + n0, XP, f, 1.f, lane);
+    }
     __syncthreads();
-    if (warp < 4) lower_left<2>(A, X, scratch, 32, 0, 8 * warp, lane);
+    {                    // the pair of blocks of 32: warp = 16 rows and 8 columns
+        const int m0 = 16 * part, n0 = 8 * quad;
+        float f[4];
+        product<4>(f, A + (32 + m0) * XP, XP, X + n0, XP, quad, 4, lane);
+        put_fragment(scratch + m0 * 8, 8, f, -1.f, lane);
+        __syncthreads();
+        product<4>(f, X + (32 + m0) * XP + 32, XP, scratch, 8, 0, part ? 4 : 2, lane);
+        put_fragment(X + (32 + m0) * XP + n0, XP, f, 1.f, lane);
+    }
     __syncthreads();
     {
         // T = inverse diag(beta) and its rows weighted, into tiles; thread = 16 columns of a row
@@ -483,17 +492,17 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
 //   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-constexpr int WC = 16;
+constexpr int WC = 16, ST = 2;      // columns of a thread; stages of loads
 
-template <int D_, int W_, int QST, int YST>
+template <int D_, int W_>
 struct Walk {
     using In = Chunk<D_>;
     static constexpr int D = D_, W = W_, PARTS = W / WC;
     static constexpr int ROW_WARPS = 4 * PARTS, THREADS = 32 * (ROW_WARPS + 2);
-    static constexpr int KQ = 2 * TILE * (D / 64), V = (In::BYTES + 1023) & ~1023, Y_STAGE = V + DC * W * 2, OFF_Y = QST * KQ;
+    static constexpr int KQ = 2 * TILE * (D / 64), V = (In::BYTES + 1023) & ~1023, Y_STAGE = V + DC * W * 2, OFF_Y = ST * KQ;
     // Operands of W columns in two terms: rows of [32 high | 32 low], or a tile of 64 high and one of 64 low columns behind each other.
     static constexpr int S_BYTES = D * 4 * W, R_BYTES = DC * 4 * W, S_LBO = D * 128, R_LBO = TILE;
-    static constexpr int OFF_S = OFF_Y + YST * Y_STAGE, OFF_R = OFF_S + S_BYTES, OFF_O = OFF_R + R_BYTES, SMEM = OFF_O + 2 * PARTS * 1024 + 1024;
+    static constexpr int OFF_S = OFF_Y + ST * Y_STAGE, OFF_R = OFF_S + S_BYTES, OFF_O = OFF_R + R_BYTES, SMEM = OFF_O + 2 * PARTS * 1024 + 1024;
     static constexpr uint32_t COL_X = 0, COL_D = 2 * W, COL_O = 4 * W, COLS = W == 32 ? 256 : 512;
     static constexpr uint32_t Y_BYTES = In::BYTES + DC * W * 2;
 };
@@ -532,14 +541,14 @@ __device__ __forceinline__ void put_split(uint8_t* tile, int lbo, int r, int par
     }
 }
 
-template <int D, int W, int QST, int YST>
-__global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
+template <int D, int W>
+__global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
                                                                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
-    using L = Walk<D, W, QST, YST>;
+    using L = Walk<D, W>;
     using In = Chunk<D>;
     constexpr int SLABS = D / W, MMA_WARP = L::ROW_WARPS, LOAD_WARP = MMA_WARP + 1;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kq_full[QST], kq_empty[QST], y_full[YST], y_empty[YST], x_full, d_full, o_full, o_free;
+    __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free;
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
@@ -549,11 +558,9 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
     const int slab = blockIdx.x % SLABS, h = (blockIdx.x / SLABS) % p.H, n = blockIdx.x / (SLABS * p.H);
 
     if (tid == 0) {
-        for (int i = 0; i < QST; ++i) {
+        for (int i = 0; i < ST; ++i) {
             mbar_init(&kq_full[i], 1);
             mbar_init(&kq_empty[i], 1);
-        }
-        for (int i = 0; i < YST; ++i) {
             mbar_init(&y_full[i], 1);
             mbar_init(&y_empty[i], 1 + L::ROW_WARPS / 2);      // the MMAs, and the warps that read the gates off the chain
         }
@@ -575,7 +582,7 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
     find_sequence(tp, n, t_begin, len, first);
     const int slot = p.slots ? p.slots[n] : n;
     const bool work = slot >= 0 && slot < p.num_slots && (len > 0 || !p.use_initial_state);
-    const int nc = work && len > 0 ? (len + DC - 1) / DC : 0;
+    const int nc = work ? (len + DC - 1) / DC : 0;
 
     if (warp == LOAD_WARP) {
         if (lane == 0 && nc > 0) {
@@ -585,28 +592,28 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
             prefetch_tensormap(&map_o);
             const int hq = h / p.group;
             for (int c = 0; c < nc && !*abortp; ++c) {
-                const int qs = c % QST, ys = c % YST;
-                if (c >= QST) WAIT(&kq_empty[qs], (c / QST - 1) & 1);
-                uint8_t* to = sm + qs * L::KQ;
-                mbar_arrive_expect_tx(&kq_full[qs], L::KQ);
+                const int st = c % ST;
+                if (c >= ST) WAIT(&kq_empty[st], (c / ST - 1) & 1);
+                uint8_t* to = sm + st * L::KQ;
+                mbar_arrive_expect_tx(&kq_full[st], L::KQ);
                 for (int half = 0; half < D / 64; ++half) {
-                    tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[qs], 0, t_begin + c * DC, half, hq);
-                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[qs], 0, t_begin + c * DC, half, hq);
+                    tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[st], 0, t_begin + c * DC, half, hq);
+                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[st], 0, t_begin + c * DC, half, hq);
                 }
-                if (c >= YST) WAIT(&y_empty[ys], (c / YST - 1) & 1);
-                to = sm + L::OFF_Y + ys * L::Y_STAGE;
-                mbar_arrive_expect_tx(&y_full[ys], L::Y_BYTES);
-                bulk_load(to, tp.ws + ((size_t)(first + c) * p.H + h) * In::BYTES, In::BYTES, &y_full[ys]);
-                tma_load_3d(to + L::V, &map_v, &y_full[ys], slab * W, h, t_begin + c * DC);
+                if (c >= ST) WAIT(&y_empty[st], (c / ST - 1) & 1);
+                to = sm + L::OFF_Y + st * L::Y_STAGE;
+                mbar_arrive_expect_tx(&y_full[st], L::Y_BYTES);
+                bulk_load(to, tp.ws + ((size_t)(first + c) * p.H + h) * In::BYTES, In::BYTES, &y_full[st]);
+                tma_load_3d(to + L::V, &map_v, &y_full[st], slab * W, h, t_begin + c * DC);
             }
         }
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
         constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1);
         for (int c = 0; c < nc; ++c) {
-            const int qs = c % QST, ys = c % YST;
-            const uint32_t kq = base + qs * L::KQ, y = base + L::OFF_Y + ys * L::Y_STAGE;
-            WAIT(&kq_full[qs], (c / QST) & 1);
+            const int st = c % ST;
+            const uint32_t kq = base + st * L::KQ, y = base + L::OFF_Y + st * L::Y_STAGE;
+            WAIT(&kq_full[st], (c / ST) & 1);
             rows_wait<1, L::ROW_WARPS>();
             tc_fence_after();
             if (elect_one()) {
@@ -614,10 +621,10 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
                 for (int kk = 0; kk < D / 16; ++kk)
                     mma_ss(tb + L::COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, L::S_LBO, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&x_full);
-                tc_commit(&kq_empty[qs]);
+                tc_commit(&kq_empty[st]);
             }
             __syncwarp();
-            WAIT(&y_full[ys], (c / YST) & 1);
+            WAIT(&y_full[st], (c / ST) & 1);
             if (c > 0) WAIT(&o_free, (c - 1) & 1);
             rows_wait<2, L::ROW_WARPS / 2>();
             tc_fence_after();
@@ -632,7 +639,7 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
                 for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
                     mma_ss(tb + L::COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, kk ? 1u : 0u);
                 tc_commit(&o_full);
-                tc_commit(&y_empty[ys]);
+                tc_commit(&y_empty[st]);
             }
             __syncwarp();
         }
@@ -690,8 +697,8 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
             }
         };
         for (int c = 0; c < nc; ++c) {
-            const int ys = c % YST, live = min(DC, len - c * DC);
-            const uint8_t* stage = sm + L::OFF_Y + ys * L::Y_STAGE;
+            const int st = c % ST, live = min(DC, len - c * DC);
+            const uint8_t* stage = sm + L::OFF_Y + st * L::Y_STAGE;
             const float* meta = reinterpret_cast<const float*>(stage + In::META);
             uint32_t a[WC], b[WC];
             float last;
@@ -700,7 +707,7 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
             tc_fence_before();
             rows_arrive<1, L::ROW_WARPS>();
             if (makes_r) {
-                WAIT_HOT(&y_full[ys], (c / YST) & 1);
+                WAIT_HOT(&y_full[st], (c / ST) & 1);
                 last = meta[2 * DC - 1];
                 const float G = -meta[DC + j];
                 uint4 vr[2];
@@ -728,11 +735,11 @@ __global__ void __launch_bounds__(Walk<D, W, QST, YST>::THREADS, 1) delta_walk_k
                 rows_arrive<2, L::ROW_WARPS / 2>();
             } else {
                 if (c > 0) outputs(c - 1);
-                WAIT_HOT(&y_full[ys], (c / YST) & 1);
+                WAIT_HOT(&y_full[st], (c / ST) & 1);
                 last = meta[2 * DC - 1];
                 const float G = meta[j];
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&y_empty[ys]);
+                if (lane == 0) mbar_arrive(&y_empty[st]);
                 WAIT_HOT(&x_full, c & 1);
                 tc_fence_after();
                 tmem_ld16(lane_addr + L::COL_X, a);
@@ -786,19 +793,19 @@ long long chunk_slots(const dsla_delta_prefill_args* a) {
     return a->cu_seqlens ? (long long)a->T_total / DC + a->N : (long long)a->N * ((a->T + DC - 1) / DC);
 }
 
-template <int D, int W, int QST, int YST>
+template <int D, int W>
 dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CUtensorMap& mq, const CUtensorMap& mo, const DeltaTcParams& tp, int T_total) {
-    using L = Walk<D, W, QST, YST>;
+    using L = Walk<D, W>;
     const DeltaParams& p = tp.p;
     CUtensorMap mv{};
     if (T_total > 0 && !make_slab_map(&mv, p.v, T_total, p.H, D, W, DC, W == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B)) return DSLA_ERR_CUDA;
     const long long ctas = (long long)p.N * p.H * (D / W);
     if (ctas > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(delta_walk_kernel<D, W, QST, YST>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
+    if (cudaFuncSetAttribute(delta_walk_kernel<D, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(L::THREADS);
     cfg.dynamicSmemBytes = L::SMEM;
-    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D, W, QST, YST>, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D, W>, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
     count_launch();
     return DSLA_OK;
 }
@@ -812,6 +819,7 @@ dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cu
         return DSLA_ERR_CUDA;
     const long long prep = a->T_total > 0 ? (long long)tp.slots * p.H : 0;
     if (prep > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(delta_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Prep<D>::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -820,20 +828,14 @@ dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cu
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (prep > 0) {
-        if (cudaFuncSetAttribute(delta_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Prep<D>::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
         cfg.gridDim = dim3((unsigned)prep);
         cfg.blockDim = dim3(PREP_THREADS);
         cfg.dynamicSmemBytes = Prep<D>::SMEM;
         if (cudaLaunchKernelEx(&cfg, delta_chunk_kernel<D>, mk, mq, tp) != cudaSuccess) return DSLA_ERR_CUDA;
         count_launch();
     }
-    static const int force = getenv("DELTA_W") ? atoi(getenv("DELTA_W")) : 0;
-    const long long units = (long long)p.N * p.H * (D / 32);
-    dsla_status rc;
-    if (force == 3212) rc = launch_walk<D, 32, 1, 2>(cfg, mk, mq, mo, tp, a->T_total);
-    else if (force == 3222 || (!force && units <= sm_count())) rc = launch_walk<D, 32, 2, 2>(cfg, mk, mq, mo, tp, a->T_total);
-    else if (force == 6412) rc = launch_walk<D, 64, 1, 2>(cfg, mk, mq, mo, tp, a->T_total);
-    else rc = launch_walk<D, 64, 2, 2>(cfg, mk, mq, mo, tp, a->T_total);
+    const dsla_status rc = (long long)p.N * p.H * (D / 32) <= sm_count() ? launch_walk<D, 32>(cfg, mk, mq, mo, tp, a->T_total)
+                                                                           : launch_walk<D, 64>(cfg, mk, mq, mo, tp, a->T_total);
     if (rc != DSLA_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? DSLA_OK : DSLA_ERR_CUDA;
 }

@@ -1,8 +1,9 @@
 // Norm of each head of queries and keys and the rotation by the token's position, one pass: rows of a projection in, rows of q and k out.
 //     y = w x r,   r = rsqrt(mean(x^2) + eps) | rsqrt(sum(x^2) + eps) | 1;      (a, b) -> (a cos f - b sin f, b cos f + a sin f)
-// A head's channels lie eight to a lane, 16-byte loads and stores; the sum of squares closes with shuffles, and so does the rotation
-// in halves (channel i meets channel i + rot/2, rot/16 lanes away).  A CTA takes the heads of one token, so the rot/2 angles and their
-// sines are computed once for all of them.  An angle is a product in fp64, reduced to half turns there: at position 100,000 an fp32 product is off by
+// A lane holds two pieces of four channels of a head, chosen so that the channels that turn with each other are its own: i and i + rot/2 (or the
+// neighbours 2i, 2i + 1), so only the sum of squares crosses lanes (with eight neighbouring channels to a lane the rotation took eight shuffles, and
+// the shuffles the time: 37 us for a 4K prompt).  A CTA takes the heads of one token: the rot/2 angles and their sines are computed once for all of them, while the
+// first heads are on their way.  An angle is a product in fp64, reduced to half turns there: at position 100,000 an fp32 product is off by
 // 4e-3 radians.  Bound by HBM: x read once, y written once.
 #include "dsla_internal.cuh"
 
@@ -12,36 +13,26 @@ namespace {
 
 constexpr int QN_THREADS = 256;
 
-template <typename T> struct Eight;
-template <> struct Eight<float> {
-    float4 a, b;
-    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-    __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    }
-    static __device__ __forceinline__ void store(float* p, const float (&x)[8]) {
-        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-    }
+// Four neighbouring channels.
+template <typename T> struct Four;
+template <> struct Four<float> {
+    float4 a;
+    __device__ __forceinline__ void zero() { a = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void get(float* x) const { x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; }
+    static __device__ __forceinline__ void store(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
 };
-template <> struct Eight<__nv_bfloat16> {
-    uint4 a;
-    __device__ __forceinline__ void zero() { a = make_uint4(0u, 0u, 0u, 0u); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+template <> struct Four<__nv_bfloat16> {
+    uint2 a;
+    __device__ __forceinline__ void zero() { a = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint2*>(p); }
+    __device__ __forceinline__ void get(float* x) const {
+        x[0] = __uint_as_float(a.x << 16); x[1] = __uint_as_float(a.x & 0xffff0000u);
+        x[2] = __uint_as_float(a.y << 16); x[3] = __uint_as_float(a.y & 0xffff0000u);
     }
-    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* x) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
+        *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
     }
 };
 
@@ -50,48 +41,48 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
     constexpr int LANES = D / 8, HEADS = QN_THREADS / LANES;      // lanes per head, heads per CTA at a time
     constexpr int AHEAD = 4;                                      // rounds of heads whose loads are issued together
     __shared__ __align__(16) float scos[D / 2], ssin[D / 2];
-    const int t = blockIdx.x, tid = threadIdx.x;
-    const int lane = tid % LANES, first = 8 * lane;
+    const int t = blockIdx.x, tid = threadIdx.x, lane = tid % LANES;
+    const int rot = p.rot, half = rot / 2;
+    const bool turns = lane < rot / 8;                            // this lane's channels turn
+    const int at0 = !INTERLEAVED && turns ? 4 * lane : 8 * lane, at1 = !INTERLEAVED && turns ? half + 4 * lane : 8 * lane + 4;
     const int begin = blockIdx.y * per, end = min(begin + per, p.H + p.H_k);      // heads of this CTA, q's first
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int rot = p.rot, half = rot / 2;
-    Eight<T> in[AHEAD];
+    Four<T> in[AHEAD][2];
     auto load = [&](int h0) {
 #pragma unroll
         for (int r = 0; r < AHEAD; ++r) {
             const int h = h0 + r * HEADS + tid / LANES;
-            if (h < end) in[r].load((h >= p.H ? reinterpret_cast<const T*>(p.k) + (size_t)t * p.k_stride + (size_t)(h - p.H) * D
-                                              : reinterpret_cast<const T*>(p.q) + (size_t)t * p.q_stride + (size_t)h * D) + first);
-            else in[r].zero();
+            if (h < end) {
+                const T* src = h >= p.H ? reinterpret_cast<const T*>(p.k) + (size_t)t * p.k_stride + (size_t)(h - p.H) * D
+                                        : reinterpret_cast<const T*>(p.q) + (size_t)t * p.q_stride + (size_t)h * D;
+                in[r][0].load(src + at0);
+                in[r][1].load(src + at1);
+            } else {
+                in[r][0].zero();
+                in[r][1].zero();
+            }
         }
     };
     load(begin);
-    // this lane's sines and cosines, with the sign that its half has: y = x cos + other sin
-    float cs[8], sn[8];
+    float wq[8], wk[8], cs[4], sn[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = (i < 4 ? at0 : at1) + (i & 3);
+        wq[i] = p.q_weight ? __ldg(p.q_weight + at) : 1.f;
+        wk[i] = p.k_weight ? __ldg(p.k_weight + at) : 1.f;
+    }
     if (rot > 0) {
         if (tid < half) {
-            const double turns = (double)p.positions[t] * (double)p.inv_freq[tid] * 0.31830988618379067154;      // half turns
-            float a, b;
-            sincospif((float)(turns - 2.0 * rint(0.5 * turns)), &a, &b);
-            scos[tid] = b;
-            ssin[tid] = a;
+            const double turned = (double)p.positions[t] * (double)p.inv_freq[tid] * 0.31830988618379067154;      // half turns
+            sincospif((float)(turned - 2.0 * rint(0.5 * turned)), &ssin[tid], &scos[tid]);
         }
         __syncthreads();
-        if (first < rot) {
+        if (turns) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int f = INTERLEAVED ? first / 2 + i / 2 : first >= half ? first - half + i : first + i;
-                cs[i] = scos[f];
-                sn[i] = (INTERLEAVED ? i % 2 == 0 : first < half) ? -ssin[f] : ssin[f];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+            for (int i = 0; i < 4; ++i) { cs[i] = scos[4 * lane + i]; sn[i] = ssin[4 * lane + i]; }
         }
     }
-    const int step = half / 8;      // lanes between the halves
-    const int partner = first < rot ? (first >= half ? (tid & 31) - step : (tid & 31) + step) : (tid & 31);
     for (int h0 = begin; h0 < end; h0 += AHEAD * HEADS) {
         if (h0 > begin) load(h0);
 #pragma unroll
@@ -100,7 +91,8 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
             const int h = h0 + r * HEADS + tid / LANES;      // heads behind the last: zeros, not stored; the shuffles run in all lanes
             const bool is_k = h >= p.H;
             float x[8];
-            in[r].get(x);
+            in[r][0].get(x);
+            in[r][1].get(x + 4);
             if (NORM != DSLA_NORM_NONE) {
                 float sum = 0.f;
 #pragma unroll
@@ -111,24 +103,22 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] *= f;
             }
-            const float* w = is_k ? p.k_weight : p.q_weight;
-            if (w) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] *= __ldg(w + first + i);
-            }
-            if (rot > 0) {
-                float other[8];
+            for (int i = 0; i < 8; ++i) x[i] *= is_k ? wk[i] : wq[i];
+            if (turns) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) other[i] = INTERLEAVED ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], partner);
-                if (first < rot) {      // channels that do not turn keep their bits
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], cs[i], other[i] * sn[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const int a = INTERLEAVED ? 2 * i : i, b = INTERLEAVED ? 2 * i + 1 : i + 4;
+                    const float u = x[a], v = x[b];
+                    x[a] = fmaf(u, cs[i], -(v * sn[i]));
+                    x[b] = fmaf(v, cs[i], u * sn[i]);
                 }
             }
             if (h < end) {
                 T* dst = is_k ? reinterpret_cast<T*>(p.k_out) + (size_t)t * p.k_out_stride + (size_t)(h - p.H) * D
                               : reinterpret_cast<T*>(p.q_out) + (size_t)t * p.q_out_stride + (size_t)h * D;
-                Eight<T>::store(dst + first, x);
+                Four<T>::store(dst + at0, x);
+                Four<T>::store(dst + at1, x + 4);
             }
         }
     }
