@@ -105,20 +105,21 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
 
 // ------------------------------------------------------------------------------------------------ Y and P T of every chunk
 // Eight warps, two to a lane quadrant (columns 0..31 and 32..63).  [K; Q] K^T is one MMA of 128 rows; quadrants 0, 1 turn its upper half into A, 2, 3 its lower half
-// into P.  (I + A)^-1 in fp32: the four diagonal blocks of 16 by substitution, one column per thread, then twice
+// into P.  (I + A)^-1 in fp32, in A's place: the eight diagonal blocks of 8 by substitution, one column per thread, then three times
 //     [a 0; b c]^-1 = [a^-1 0; -c^-1 b a^-1 c^-1]
-// for pairs of blocks of 16 and of 32, columns eight to a warp, as TF32 products of two terms each (22 bits).  Then Y and P T are MMAs.  (A substitution over all 64
-// rows by 64 threads, 2016 steps of the chain each, and T written two bytes at a time took 110 us for 4096 tokens of 32 heads.)
+// for pairs of blocks of 8, 16 and 32, columns eight to a warp, as TF32 products of two terms each (22 bits).  Then P T and Y are MMAs, one after the other through
+// the same tiles: 56 KB and 64 registers a thread keep four CTAs on an SM.  4096 tokens of 32 heads: 52 us with 75 KB and three CTAs; 110 us with a substitution over
+// all 64 rows by 64 threads, 2016 steps of the chain each, and T written two bytes at a time.
 constexpr int PREP_THREADS = 256;
-constexpr int XP = 68;                                          // pitch of A and of the inverse in shared memory, floats
-constexpr int PREP_A = 0, PREP_X = DC * XP * 4, PREP_SCRATCH = 2 * PREP_X;      // behind K and Q; scratch: [32][8] floats of four warps
-constexpr int PREP_T = 0, PREP_W = 2 * TILE;                    // the same room later: T in two terms, diag(2^(L_63 - L)) T in three
-constexpr int PREP_WORK = 5 * TILE;
-static_assert(PREP_SCRATCH + 4 * 32 * 8 * 4 <= PREP_WORK, "A, the inverse and the scratch fit where T will be");
+constexpr int XP = 68;                                          // pitch of A and its inverse in shared memory, floats
+constexpr int PREP_A = 0, PREP_SCRATCH = DC * XP * 4;           // behind K and Q; scratch: [32][8] floats of four pairs of warps
+constexpr int PREP_T = 0;                                       // the same room later: T in two terms, then two of the three terms of diag(2^(L_63 - L)) T, then P T
+constexpr int PREP_WORK = PREP_SCRATCH + 4 * 32 * 8 * 4;
+static_assert(PREP_WORK >= 2 * TILE && PREP_WORK % 1024 == 0, "two tiles fit where A and the scratch are");
 
 template <int D>
 struct Prep {
-    // P's high terms take the place of Q's first tile, the low ones that of its second (d = 64 has none: one more)
+    // P's high terms take the place of Q's first tile, the low ones that of its second (d = 64 has none: one more), the third term of the weighted T theirs
     static constexpr int KQ = 2 * TILE * (D / 64), P_LO = D == 128 ? 3 * TILE : KQ + PREP_WORK;
     static constexpr int META = KQ + PREP_WORK + (D == 128 ? 0 : TILE), SMEM = META + 2 * DC * 4 + 1024;
 };
@@ -161,7 +162,7 @@ __device__ __forceinline__ void put_fragment(float* M, int pitch, const float (&
 }
 
 template <int D>
-__global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const DeltaTcParams tp) {
+__global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const DeltaTcParams tp) {
     using L = Prep<D>;
     using Out = Chunk<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -276,7 +277,6 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
     const int quad = warp & 3, part = warp >> 2, row = 32 * quad + lane, j = row & 63, upper = quad & 1;
     const uint32_t row_addr = tb + ((uint32_t)(32 * quad) << 16) + 32 * part;
     float* A = reinterpret_cast<float*>(work + PREP_A);
-    float* X = reinterpret_cast<float*>(work + PREP_X);
     const bool is_p = quad >= 2;
     WAIT(&done, 0);
     tc_fence_after();
@@ -285,48 +285,44 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) *reinterpret_cast<uint4*>(sm + half * 2 * TILE + i * 16) = make_uint4(0u, 0u, 0u, 0u);
     if (upper >= part) {
-        float x[32];
-        {
-            uint32_t r[32];
-            tmem_ld32(row_addr, r);
+        const float f = j < live ? (is_p ? p.scale : sbeta[j]) : 0.f, hj = lhi[j], lj = llo[j];
+        const float fr = f * ex2((hj - lhi[31]) + (lj - llo[31]));      // left of a diagonal block of 32: through the sum up to token 31
+        const int last = j >= live ? -1 : is_p ? j : j - 1;             // columns up to this one
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int c0 = 32 * part + 16 * half;
+            uint32_t r[16];
+            float x[16];
+            tmem_ld16(row_addr + 16 * half, r);
             tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
-        }
-        const float f = j < live ? (is_p ? p.scale : sbeta[j]) : 0.f;
-        if (upper == part) {      // a diagonal block of 32
-            const float hj = lhi[j], lj = llo[j];
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const float4 hs = *reinterpret_cast<const float4*>(lhi + 32 * part + i), ls = *reinterpret_cast<const float4*>(llo + 32 * part + i);
-                x[i] *= f * ex2((hj - hs.x) + (lj - ls.x));
-                x[i + 1] *= f * ex2((hj - hs.y) + (lj - ls.y));
-                x[i + 2] *= f * ex2((hj - hs.z) + (lj - ls.z));
-                x[i + 3] *= f * ex2((hj - hs.w) + (lj - ls.w));
+            for (int i = 0; i < 16; i += 4) {
+                float4 e;
+                if (upper == part) {
+                    const float4 hs = *reinterpret_cast<const float4*>(lhi + c0 + i), ls = *reinterpret_cast<const float4*>(llo + c0 + i);
+                    e = make_float4(f * ex2((hj - hs.x) + (lj - ls.x)), f * ex2((hj - hs.y) + (lj - ls.y)), f * ex2((hj - hs.z) + (lj - ls.z)), f * ex2((hj - hs.w) + (lj - ls.w)));
+                } else {
+                    const float4 l = *reinterpret_cast<const float4*>(sleft + c0 + i);
+                    e = make_float4(fr * l.x, fr * l.y, fr * l.z, fr * l.w);
+                }
+                x[i] = c0 + i <= last ? __uint_as_float(r[i]) * e.x : 0.f;
+                x[i + 1] = c0 + i + 1 <= last ? __uint_as_float(r[i + 1]) * e.y : 0.f;
+                x[i + 2] = c0 + i + 2 <= last ? __uint_as_float(r[i + 2]) * e.z : 0.f;
+                x[i + 3] = c0 + i + 3 <= last ? __uint_as_float(r[i + 3]) * e.w : 0.f;
             }
-        } else {                  // left of it: through the sum up to token 31
-            const float fr = f * ex2((lhi[j] - lhi[31]) + (llo[j] - llo[31]));
+            if (!is_p) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const float4 l = *reinterpret_cast<const float4*>(sleft + i);
-                x[i] *= fr * l.x; x[i + 1] *= fr * l.y; x[i + 2] *= fr * l.z; x[i + 3] *= fr * l.w;
-            }
-        }
-        const int last = j >= live ? -1 : is_p ? j : j - 1;      // columns up to this one
+                for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(A + j * XP + c0 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = 32 * part + i <= last ? x[i] : 0.f;
-        if (!is_p) {
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(A + j * XP + 32 * part + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], hi[e], lo[e]);
-                const int at16 = j * 128 + (((4 * part + i) ^ (j & 7)) << 4);
-                *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], hi[e], lo[e]);
+                    const int at16 = j * 128 + (((c0 / 8 + i) ^ (j & 7)) << 4);
+                    *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
             }
         }
     } else if (is_p) {
@@ -339,134 +335,183 @@ __global__ void __launch_bounds__(PREP_THREADS, 3) delta_chunk_kernel(const __gr
     }
     tc_fence_before();
     __syncthreads();
-    if (warp < 2) {      // diagonal blocks of 16: thread = column
-        const int b0 = 16 * (tid >> 4), col = tid & 15;
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float s[4] = {i == col ? 1.f : 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < i; k += 4) {
-                const float4 a = *reinterpret_cast<const float4*>(A + (b0 + i) * XP + b0 + k);
-                s[0] = fmaf(-a.x, x[k], s[0]);
-                if (k + 1 < i) s[1] = fmaf(-a.y, x[k + 1], s[1]);
-                if (k + 2 < i) s[2] = fmaf(-a.z, x[k + 2], s[2]);
-                if (k + 3 < i) s[3] = fmaf(-a.w, x[k + 3], s[3]);
-            }
-            x[i] = (s[0] + s[1]) + (s[2] + s[3]);
-            X[(b0 + i) * XP + b0 + col] = x[i];
-        }
-    } else if (warp < 4) {      // right of the diagonal blocks the products read zeros
-        const int i = tid - 64;
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<float4*>(X + (32 * k + (i >> 2)) * XP + 32 * k + 16 + 4 * (i & 3)) = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    __syncthreads();
     float* scratch = reinterpret_cast<float*>(work + PREP_SCRATCH) + (warp & 3) * 256;      // [rows][8] of this warp's, or this pair's, columns
-    if (warp < 4) {      // pairs of blocks of 16: warp = pair and 8 columns
-        const int r0 = 32 * (warp >> 1) + 16, c0 = r0 - 16, n0 = 8 * (warp & 1);
-        float f[4];
-        product<2>(f, A + r0 * XP + c0, XP, X + c0 * XP + c0 + n0, XP, n0 / 8, 2, lane);
-        put_fragment(scratch, 8, f, -1.f, lane);
+    const int fr_ = lane >> 2, fq = lane & 3;
+    if (warp < 4) {
+        const int b0 = 16 * warp;
+        if (lane < 16) {      // two blocks of 8: thread = column
+            const int at8 = b0 + (lane & 8), col = lane & 7;
+            float4 a[10];      // rows 1 .. 7 left of the diagonal
+#pragma unroll
+            for (int i = 1; i < 8; ++i) {
+                a[i < 5 ? i - 1 : 2 * i - 6] = *reinterpret_cast<const float4*>(A + (at8 + i) * XP + at8);
+                if (i >= 5) a[2 * i - 5] = *reinterpret_cast<const float4*>(A + (at8 + i) * XP + at8 + 4);
+            }
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float s0 = i == col ? 1.f : 0.f, s1 = 0.f;
+                if (i > 0) {
+                    const float4 l = a[i < 5 ? i - 1 : 2 * i - 6];
+                    s0 = fmaf(-l.x, x[0], s0);
+                    if (i > 1) s1 = fmaf(-l.y, x[1], s1);
+                    if (i > 2) s0 = fmaf(-l.z, x[2], s0);
+                    if (i > 3) s1 = fmaf(-l.w, x[3], s1);
+                    if (i > 4) {
+                        const float4 u = a[2 * i - 5];
+                        s0 = fmaf(-u.x, x[4], s0);
+                        if (i > 5) s1 = fmaf(-u.y, x[5], s1);
+                        if (i > 6) s0 = fmaf(-u.z, x[6], s0);
+                    }
+                }
+                x[i] = s0 + s1;
+            }
+            __syncwarp(0xffffu);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) A[(at8 + i) * XP + at8 + col] = x[i];
+        }
         __syncwarp();
-        product<2>(f, X + r0 * XP + r0, XP, scratch, 8, 0, 2, lane);
-        put_fragment(X + r0 * XP + c0 + n0, XP, f, 1.f, lane);
-    }
-    __syncthreads();
-    {                    // the pair of blocks of 32: warp = 16 rows and 8 columns
-        const int m0 = 16 * part, n0 = 8 * quad;
+        // the pair of them (rows 8..15 of the fragments are whatever lies below)
         float f[4];
-        product<4>(f, A + (32 + m0) * XP, XP, X + n0, XP, quad, 4, lane);
-        put_fragment(scratch + m0 * 8, 8, f, -1.f, lane);
-        __syncthreads();
-        product<4>(f, X + (32 + m0) * XP + 32, XP, scratch, 8, 0, part ? 4 : 2, lane);
-        put_fragment(X + (32 + m0) * XP + n0, XP, f, 1.f, lane);
+        product<1>(f, A + (b0 + 8) * XP + b0, XP, A + b0 * XP + b0, XP, 0, 1, lane);
+        *reinterpret_cast<float2*>(scratch + fr_ * 8 + 2 * fq) = make_float2(-f[0], -f[1]);
+        __syncwarp();
+        product<1>(f, A + (b0 + 8) * XP + b0 + 8, XP, scratch, 8, 0, 1, lane);
+        *reinterpret_cast<float2*>(A + (b0 + 8 + fr_) * XP + b0 + 2 * fq) = make_float2(f[0], f[1]);
     }
     __syncthreads();
     {
-        // T = inverse diag(beta) and its rows weighted, into tiles; thread = 16 columns of a row
-        const int s = tid >> 2, c0 = 16 * (tid & 3);
+        // pairs of blocks of 16: warp = pair and 8 columns
+        const int r0 = 32 * ((warp >> 1) & 1) + 16, c0 = r0 - 16, n0 = 8 * (warp & 1);
+        float f[4];
+        if (warp < 4) {
+            product<2>(f, A + r0 * XP + c0, XP, A + c0 * XP + c0 + n0, XP, n0 / 8, 2, lane);
+            put_fragment(scratch, 8, f, -1.f, lane);
+        }
+        __syncthreads();
+        if (warp < 4) {
+            product<2>(f, A + r0 * XP + r0, XP, scratch, 8, 0, 2, lane);
+            put_fragment(A + r0 * XP + c0 + n0, XP, f, 1.f, lane);
+        }
+    }
+    __syncthreads();
+    {
+        // the pair of blocks of 32: warp = 16 rows and 8 columns
+        const int m0 = 16 * part, n0 = 8 * quad;
+        float f[4];
+        product<4>(f, A + (32 + m0) * XP, XP, A + n0, XP, quad, 4, lane);
+        put_fragment(scratch + m0 * 8, 8, f, -1.f, lane);
+        __syncthreads();
+        product<4>(f, A + (32 + m0) * XP + 32, XP, scratch, 8, 0, part ? 4 : 2, lane);
+        put_fragment(A + (32 + m0) * XP + n0, XP, f, 1.f, lane);
+    }
+    __syncthreads();
+    // T = inverse diag(beta) into tiles, then with its rows weighted; thread = 16 columns of a row
+    const int ts = tid >> 2, tc0 = 16 * (tid & 3);
+    uint8_t* const t_at = work + PREP_T + ts * 128;
+    uint32_t w[3][8];
+    {
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float4 y = *reinterpret_cast<const float4*>(X + s * XP + c0 + i), b = *reinterpret_cast<const float4*>(sbeta + c0 + i);
-            x[i] = c0 + i <= s ? y.x * b.x : 0.f;
-            x[i + 1] = c0 + i + 1 <= s ? y.y * b.y : 0.f;
-            x[i + 2] = c0 + i + 2 <= s ? y.z * b.z : 0.f;
-            x[i + 3] = c0 + i + 3 <= s ? y.w * b.w : 0.f;
+            const float4 y = *reinterpret_cast<const float4*>(A + ts * XP + tc0 + i), b = *reinterpret_cast<const float4*>(sbeta + tc0 + i);
+            x[i] = tc0 + i <= ts ? y.x * b.x : 0.f;
+            x[i + 1] = tc0 + i + 1 <= ts ? y.y * b.y : 0.f;
+            x[i + 2] = tc0 + i + 2 <= ts ? y.z * b.z : 0.f;
+            x[i + 3] = tc0 + i + 3 <= ts ? y.w * b.w : 0.f;
         }
-        const float w = sw[s];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            uint32_t t[2][4], y[3][4];
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float u = x[8 * i + 2 * e], v = x[8 * i + 2 * e + 1];
-                split2(u, v, t[0][e], t[1][e]);
-                const float uw = u * w, vw = v * w;
-                y[0][e] = pack_bf16(uw, vw);
-                const float2 hi = unpack_bf16(y[0][e]);
-                split2(uw - hi.x, vw - hi.y, y[1][e], y[2][e]);
-            }
-            uint8_t* to = work + s * 128 + (((c0 / 8 + i) ^ (s & 7)) << 4);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(to + PREP_T + k * TILE) = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to + PREP_W + k * TILE) = make_uint4(y[k][0], y[k][1], y[k][2], y[k][3]);
+            for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], hi[e], lo[e]);
+            const int piece = ((tc0 / 8 + i) ^ (ts & 7)) << 4;
+            *reinterpret_cast<uint4*>(t_at + piece) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(t_at + TILE + piece) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
+        fence_proxy_async_smem();
+        __syncthreads();
+        if (warp == 0 && elect_one()) {
+            tc_fence_after();
+            // P T cancels where keys are alike (its rows are differences of P's), so both factors keep two terms.  Rows 64..127 of the operands are P; the
+            // products of the 64 rows before them are not read.
+            constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
+            const uint32_t tt = smem_u32(work + PREP_T), p_hi = smem_u32(sm), p_lo = smem_u32(sm + L::P_LO - TILE);
+#pragma unroll
+            for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_lo + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
+#pragma unroll
+            for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + TILE + kk * 2048, 16, 1024), ID, 1u);
+#pragma unroll
+            for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID, 1u);
+            tc_commit(&done);
+        }
+        __syncwarp();
+        const float weight = sw[ts];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float u = x[2 * i] * weight, v = x[2 * i + 1] * weight;
+            w[0][i] = pack_bf16(u, v);
+            const float2 hi = unpack_bf16(w[0][i]);
+            split2(u - hi.x, v - hi.y, w[1][i], w[2][i]);
+        }
+    }
+    WAIT(&done, 1);
+    tc_fence_after();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int piece = ((tc0 / 8 + i) ^ (ts & 7)) << 4;
+        *reinterpret_cast<uint4*>(t_at + piece) = make_uint4(w[0][4 * i], w[0][4 * i + 1], w[0][4 * i + 2], w[0][4 * i + 3]);
+        *reinterpret_cast<uint4*>(t_at + TILE + piece) = make_uint4(w[1][4 * i], w[1][4 * i + 1], w[1][4 * i + 2], w[1][4 * i + 3]);
+        *reinterpret_cast<uint4*>(sm + L::P_LO + ts * 128 + piece) = make_uint4(w[2][4 * i], w[2][4 * i + 1], w[2][4 * i + 2], w[2][4 * i + 3]);
     }
     fence_proxy_async_smem();
     __syncthreads();
     if (warp == 0 && elect_one()) {
         tc_fence_after();
-        const uint32_t kt = smem_u32(sm), tt = smem_u32(work + PREP_T), wt = smem_u32(work + PREP_W);
-        // Y: d = 64 has 64 rows, the other half of the product is not read
-        constexpr uint32_t ID_Y = idesc_bf16(128, 64, 1, 1), ID_P = idesc_bf16(128, 64, 0, 1);
+        constexpr uint32_t ID = idesc_bf16(128, 64, 1, 1);      // d = 64 has 64 rows, the other half of the product is not read
+        const uint32_t kt = smem_u32(sm), wt = smem_u32(work + PREP_T), w2 = smem_u32(sm + L::P_LO);
 #pragma unroll
         for (int k = 2; k >= 0; --k)
 #pragma unroll
             for (int kk = 0; kk < DC / 16; ++kk)
-                mma_ss(tb + 64, smem_desc_sw128(kt + kk * 2048, 2 * TILE, 1024), smem_desc_sw128(wt + k * TILE + kk * 2048, 16, 1024), ID_Y, k < 2 || kk ? 1u : 0u);
-        // P T cancels where keys are alike (its rows are differences of P's), so both factors keep two terms.  Rows 64..127 of the operands are P; the
-        // products of the 64 rows before them are not read.
-        const uint32_t p_hi = smem_u32(sm), p_lo = smem_u32(sm + L::P_LO - TILE);
-#pragma unroll
-        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_lo + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID_P, kk ? 1u : 0u);
-#pragma unroll
-        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + TILE + kk * 2048, 16, 1024), ID_P, 1u);
-#pragma unroll
-        for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID_P, 1u);
+                mma_ss(tb + 64, smem_desc_sw128(kt + kk * 2048, 2 * TILE, 1024), smem_desc_sw128((k == 2 ? w2 : wt + k * TILE) + kk * 2048, 16, 1024), ID, k < 2 || kk ? 1u : 0u);
         tc_commit(&done);
     }
     __syncwarp();
-    WAIT(&done, 1);
-    tc_fence_after();
-    if (row < D) {      // Y where K and P were
-        uint32_t r[32];
-        tmem_ld32(row_addr + 64, r);
-        tc_wait_ld();
+    uint32_t pt[16];
+    if (is_p) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t hi[4], lo[4];
+        for (int half = 0; half < 2; ++half) {
+            uint32_t r[16];
+            tmem_ld16(row_addr + 16 * half, r);
+            tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) split2(__uint_as_float(r[8 * i + 2 * e]), __uint_as_float(r[8 * i + 2 * e + 1]), hi[e], lo[e]);
-            const int at16 = row * 128 + (((4 * part + i) ^ (row & 7)) << 4);
-            *reinterpret_cast<uint4*>(sm + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(sm + Out::Y + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            for (int i = 0; i < 8; ++i) pt[8 * half + i] = pack_bf16(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
         }
     }
+    WAIT(&done, 0);
+    tc_fence_after();
     if (is_p) {         // P T where T was
-        uint32_t r[32];
-        tmem_ld32(row_addr, r);
-        tc_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w[4];
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(work + PREP_T + j * 128 + (((4 * part + i) ^ (j & 7)) << 4)) = make_uint4(pt[4 * i], pt[4 * i + 1], pt[4 * i + 2], pt[4 * i + 3]);
+    }
+    if (row < D) {      // Y where K and P were
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__uint_as_float(r[8 * i + 2 * e]), __uint_as_float(r[8 * i + 2 * e + 1]));
-            *reinterpret_cast<uint4*>(work + PREP_T + j * 128 + (((4 * part + i) ^ (j & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int half = 0; half < 2; ++half) {
+            uint32_t r[16];
+            tmem_ld16(row_addr + 64 + 16 * half, r);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) split2(__uint_as_float(r[8 * i + 2 * e]), __uint_as_float(r[8 * i + 2 * e + 1]), hi[e], lo[e]);
+                const int at16 = row * 128 + (((4 * part + 2 * half + i) ^ (row & 7)) << 4);
+                *reinterpret_cast<uint4*>(sm + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4*>(sm + Out::Y + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
         }
     }
     fence_proxy_async_smem();
@@ -550,12 +595,13 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free;
     __shared__ uint32_t tmem_base;
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, sequence;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
     const DeltaParams& p = tp.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abortp = &abort_flag;
-    const int slab = blockIdx.x % SLABS, h = (blockIdx.x / SLABS) % p.H, n = blockIdx.x / (SLABS * p.H);
+    const int slab = blockIdx.x % SLABS, h = (blockIdx.x / SLABS) % p.H;
+    int n = blockIdx.x / (SLABS * p.H);
 
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
@@ -578,6 +624,20 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     const uint32_t tb = tmem_base;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (p.cu_seqlens && p.N > 1 && p.N <= 128) {      // the longest sequences first (58K tokens in 16 sequences of 1 to 8K: xx ms in the order given)
+        if (tid < p.N) {
+            const int mine = p.cu_seqlens[tid + 1] - p.cu_seqlens[tid];
+            int rank = 0, from = p.cu_seqlens[0];
+            for (int k = 0; k < p.N; ++k) {
+                const int to = p.cu_seqlens[k + 1], other = to - from;
+                rank += other > mine || (other == mine && k < tid);
+                from = to;
+            }
+            if (rank == n) sequence = tid;
+        }
+        __syncthreads();
+        n = sequence;
+    }
     int t_begin, len, first;
     find_sequence(tp, n, t_begin, len, first);
     const int slot = p.slots ? p.slots[n] : n;
