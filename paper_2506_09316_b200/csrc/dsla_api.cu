@@ -455,7 +455,7 @@ dsla_status dsla_delta_prefill(const dsla_delta_prefill_args* a, dsla_state* st,
     p.N = a->N; p.T = a->T; p.H = a->H; p.group = a->H / a->H_qk; p.num_slots = st->num_slots;
     p.use_initial_state = a->use_initial_state ? 1 : 0; p.scale = a->scale;
     if (delta_on_tensor_cores(a)) return launch_delta_tc(p, a, static_cast<cudaStream_t>(cuda_stream));
-    return launch_delta_recurrent(p, a->d_k, a->dtype, static_cast<cudaStream_t>(cuda_stream));
+    return launch_delta_simt(p, a->d_k, a->dtype, static_cast<cudaStream_t>(cuda_stream));
 }
 
 dsla_status dsla_delta_decode_step(const dsla_delta_decode_args* a, dsla_state* st, void* cuda_stream) {

@@ -12,7 +12,7 @@
 // it, with rounding.  P T, which reaches only the bf16 output, has one term.
 #include <cuda.h>
 
-#include "dsla_internal.cuh"
+#include "dsla_delta.cuh"
 #include "tc_utils.cuh"
 
 namespace dsla {
@@ -66,34 +66,6 @@ __device__ __forceinline__ void find_sequence(const DeltaTcParams& tp, int n, in
     }
 }
 
-// Pairs of fp32: one instruction for two.
-__device__ __forceinline__ uint64_t pair(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ uint64_t pair(uint32_t x, uint32_t y) { return pair(__uint_as_float(x), __uint_as_float(y)); }
-__device__ __forceinline__ float2 unpair(uint64_t x) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
-    return r;
-}
-
 // x in two bf16 terms, high and low.
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
     hi = pack_bf16(x, y);
@@ -123,43 +95,6 @@ struct Prep {
     static constexpr int KQ = 2 * TILE * (D / 64), P_LO = D == 128 ? 3 * TILE : KQ + PREP_WORK;
     static constexpr int META = KQ + PREP_WORK + (D == 128 ? 0 : TILE), SMEM = META + 2 * DC * 4 + 1024;
 };
-
-__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
-}
-__device__ __forceinline__ void tf32_terms(float x, uint32_t& hi, uint32_t& lo) {
-    hi = __float_as_uint(x) & 0xffffe000u;
-    lo = __float_as_uint(x - __uint_as_float(hi));
-}
-// 16 rows of M[16 x 8 KT] B[8 KT x 8], both in shared memory (row pitches pa, pb), as products of two TF32 terms; steps of 8 from k_first up to k_last - 1.
-template <int KT>
-__device__ __forceinline__ void product(float (&c)[4], const float* M, int pa, const float* B, int pb, int k_first, int k_last, int lane) {
-    const int r = lane >> 2, q = lane & 3;
-    float c1[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};      // (three sums side by side: an MMA waits 35 cycles for the one before it)
-    c[0] = c[1] = c[2] = c[3] = 0.f;
-#pragma unroll
-    for (int k = 0; k < KT; ++k) {
-        if (k < k_first || k >= k_last) continue;
-        uint32_t ah[4], al[4], bh[2], bl[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) tf32_terms(B[(8 * k + q + 4 * i) * pb + r], bh[i], bl[i]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tf32_terms(M[(r + 8 * (i & 1)) * pa + 8 * k + q + 4 * (i >> 1)], ah[i], al[i]);
-        mma_tf32(c1, al, bh);
-        mma_tf32(c2, ah, bl);
-        mma_tf32(c, ah, bh);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] += c1[i] + c2[i];
-}
-// A 16 x 8 fragment to rows r0 .. of a matrix of pitch `pitch`, scaled.
-__device__ __forceinline__ void put_fragment(float* M, int pitch, const float (&c)[4], float f, int lane) {
-    const int r = lane >> 2, q = lane & 3;
-    *reinterpret_cast<float2*>(M + r * pitch + 2 * q) = make_float2(f * c[0], f * c[1]);
-    *reinterpret_cast<float2*>(M + (r + 8) * pitch + 2 * q) = make_float2(f * c[2], f * c[3]);
-}
 
 template <int D>
 __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const DeltaTcParams tp) {
@@ -373,10 +308,10 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         __syncwarp();
         // the pair of them (rows 8..15 of the fragments are whatever lies below)
         float f[4];
-        product<1>(f, A + (b0 + 8) * XP + b0, XP, A + b0 * XP + b0, XP, 0, 1, lane);
+        product<1>(f, A + (b0 + 8) * XP + b0, XP, 1, A + b0 * XP + b0, XP, 1, 0, 1, lane);
         *reinterpret_cast<float2*>(scratch + fr_ * 8 + 2 * fq) = make_float2(-f[0], -f[1]);
         __syncwarp();
-        product<1>(f, A + (b0 + 8) * XP + b0 + 8, XP, scratch, 8, 0, 1, lane);
+        product<1>(f, A + (b0 + 8) * XP + b0 + 8, XP, 1, scratch, 8, 1, 0, 1, lane);
         *reinterpret_cast<float2*>(A + (b0 + 8 + fr_) * XP + b0 + 2 * fq) = make_float2(f[0], f[1]);
     }
     __syncthreads();
@@ -385,12 +320,12 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         const int r0 = 32 * ((warp >> 1) & 1) + 16, c0 = r0 - 16, n0 = 8 * (warp & 1);
         float f[4];
         if (warp < 4) {
-            product<2>(f, A + r0 * XP + c0, XP, A + c0 * XP + c0 + n0, XP, n0 / 8, 2, lane);
+            product<2>(f, A + r0 * XP + c0, XP, 1, A + c0 * XP + c0 + n0, XP, 1, n0 / 8, 2, lane);
             put_fragment(scratch, 8, f, -1.f, lane);
         }
         __syncthreads();
         if (warp < 4) {
-            product<2>(f, A + r0 * XP + r0, XP, scratch, 8, 0, 2, lane);
+            product<2>(f, A + r0 * XP + r0, XP, 1, scratch, 8, 1, 0, 2, lane);
             put_fragment(A + r0 * XP + c0 + n0, XP, f, 1.f, lane);
         }
     }
@@ -399,10 +334,10 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         // the pair of blocks of 32: warp = 16 rows and 8 columns
         const int m0 = 16 * part, n0 = 8 * quad;
         float f[4];
-        product<4>(f, A + (32 + m0) * XP, XP, A + n0, XP, quad, 4, lane);
+        product<4>(f, A + (32 + m0) * XP, XP, 1, A + n0, XP, 1, quad, 4, lane);
         put_fragment(scratch + m0 * 8, 8, f, -1.f, lane);
         __syncthreads();
-        product<4>(f, A + (32 + m0) * XP + 32, XP, scratch, 8, 0, part ? 4 : 2, lane);
+        product<4>(f, A + (32 + m0) * XP + 32, XP, 1, scratch, 8, 1, 0, part ? 4 : 2, lane);
         put_fragment(A + (32 + m0) * XP + n0, XP, f, 1.f, lane);
     }
     __syncthreads();

@@ -91,9 +91,9 @@ dsla_status launch_decode(const DecodeParams& p, int d, dsla_dtype dt, cudaStrea
 dsla_status launch_state_copy(const dsla_state* st, const int32_t* src, const int32_t* dst, int n, cudaStream_t s);
 // dsla_qk_norm.cu
 dsla_status launch_qk_norm_rope(const dsla_qk_norm_rope_args* a, cudaStream_t s);
-// dsla_delta_decode.cu, dsla_delta_recurrent.cu, dsla_delta_tc.cu
+// dsla_delta_decode.cu, dsla_delta_simt.cu, dsla_delta_tc.cu
 dsla_status launch_delta_decode(const DeltaParams& p, int d, dsla_dtype dt, cudaStream_t s);
-dsla_status launch_delta_recurrent(const DeltaParams& p, int d, dsla_dtype dt, cudaStream_t s);
+dsla_status launch_delta_simt(const DeltaParams& p, int d, dsla_dtype dt, cudaStream_t s);
 size_t delta_tc_workspace_bytes(const dsla_delta_prefill_args* a);
 dsla_status launch_delta_tc(const DeltaParams& p, const dsla_delta_prefill_args* a, cudaStream_t s);
 // dsla_gate_project.cu
