@@ -1,6 +1,6 @@
 // Gated delta rule over prompts in fp32, in chunks of 16 tokens (dsla_delta_tc.cu has the chunk's formulas):
 //     R = V - G K S,       O = scale G Q S + (P T) R,       S <- G_15 S + Y R,       Y = K^T diag(D_15) T,   T = (I + A)^-1 diag(beta).
-// A CTA owns (sequence, head, 16 columns of d_v).  Four warps walk the chunks, four others make Y and P T of the next chunk meanwhile and fetch the one after.  The products with
+// A CTA owns (sequence, head, 16 columns of d_v).  Four warps walk the chunks; three groups of four make Y and P T of the chunks ahead in turn, and fetch their next one meanwhile.  The products with
 // d_k or a chunk in their middle run as TF32 products of two terms (22 bits, fp32 sums): with plain FMAs each operand is read from shared memory as often as it is used, and the
 // reads took 5600 cycles a chunk.  The state is fp32 in the accumulators' layout, one copy of it in shared memory for K S and Q S.  Products of gates are plain products: a gate of 0 is
 // exact.  Tokens behind a sequence's end have no key, no beta and a gate of 1: they change nothing.
@@ -12,7 +12,7 @@ namespace dsla {
 
 namespace {
 
-constexpr int DS_C = 16, DS_COLS = 16, DS_THREADS = 256;
+constexpr int DS_C = 16, DS_COLS = 16, DS_GROUPS = 3, DS_THREADS = 128 * (1 + DS_GROUPS), DS_BUFFERS = DS_GROUPS + 1;
 
 // Four consecutive elements as fp32.
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -31,21 +31,23 @@ struct DeltaChunk {
 };
 // What the preparation keeps to itself.
 struct DeltaWork {
-    float decay[DS_C][DS_C + 1];          // D_ji
     float a[DS_C][DS_C + 4], p[DS_C][DS_C + 4], t[DS_C][DS_C + 4], wt[DS_C][DS_C + 8], x[8][9];
-    float gate[DS_C], beta[DS_C];
+    float power[4][DS_C];                 // products of 1, 2, 4, 8 gates, the last that of token j
+    float beta[DS_C], left[DS_C];         // left: D_15,j
 };
 template <int D>
 struct DeltaShared {
     static constexpr int SP = DS_COLS + 8;
-    DeltaChunk<D> chunk[2];
-    DeltaWork work;
+    DeltaChunk<D> chunk[DS_BUFFERS];
+    DeltaWork work[DS_GROUPS];
     float s[D][SP];                       // the state that the chunk starts from
     float r[DS_C][SP];                    // R
 };
 
-#define PREP_SYNC() asm volatile("bar.sync 1, 128;" ::: "memory")
-#define WALK_SYNC() asm volatile("bar.sync 2, 128;" ::: "memory")
+// Named barriers: 1 + group within the preparing groups, 4 within the walk; 5 + b: buffer b is ready (its group arrives, the walk waits), 9 + b: it has been walked.
+__device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pass_arrive(int id) { asm volatile("bar.arrive %0, 256;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pass_wait(int id) { asm volatile("bar.sync %0, 256;" ::"r"(id) : "memory"); }
 
 template <int D, typename T>
 __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParams p) {
@@ -66,9 +68,10 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
     const int chunks = len > 0 ? (len + DS_C - 1) / DS_C : 0;
 
     if (warp >= 4) {
-        // ---------------------------------------------------------------- preparation: chunk c + 1 while the walk is at chunk c
-        const int u = tid - 128, Hqk = p.H / p.group, hq = h / p.group;
-        DeltaWork& w = sh.work;
+        // ---------------------------------------------------------------- preparation of every third chunk
+        const int group = (warp - 4) >> 2, u = tid & 127, pw = warp & 3, Hqk = p.H / p.group, hq = h / p.group;
+        const int i8 = 8 * (pw & 1), fr = lane >> 2, fq = lane & 3;
+        DeltaWork& w = sh.work[group];
         float4 rq[LOADS], rk[LOADS], rv;
         float rg = 1.f, rb = 0.f;
         auto fetch = [&](int c) {
@@ -92,10 +95,11 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
                 rb = t < len ? p.beta[(size_t)(t_begin + t) * p.H + h] : 0.f;
             }
         };
-        fetch(0);
-        for (int c = 0; c <= chunks; ++c) {
-            if (c < chunks) {
-                DeltaChunk<D>& ch = sh.chunk[c & 1];
+        fetch(group);
+        for (int c = group; c < chunks; c += DS_GROUPS) {
+            DeltaChunk<D>& ch = sh.chunk[c % DS_BUFFERS];
+            {
+                if (c >= DS_BUFFERS) pass_wait(9 + c % DS_BUFFERS);
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i) {
                     const int e = (i * 128 + u) * 4;
@@ -103,52 +107,81 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
                     *reinterpret_cast<float4*>(&ch.kq[e / D][e % D]) = rk[i];
                 }
                 if (u < 64) *reinterpret_cast<float4*>(&ch.v[u / 4][(u & 3) * 4]) = rv;
-                else if (u < 64 + DS_C) {
-                    w.gate[u - 64] = rg < 0.f ? 0.f : rg;
-                    w.beta[u - 64] = rb;
-                }
-                fetch(c + 1);
-                PREP_SYNC();
-                if (u >= 96 && u < 96 + DS_C) {      // row j of the gates' products
-                    const int j = u - 96;
-                    float d = 1.f;
-                    for (int i = j; i >= 0; --i) {
-                        w.decay[j][i] = d;
-                        d *= w.gate[i];
+                else if (u < 96) {      // (one warp: lanes 0..15 have the gates)
+                    const float one = rg < 0.f ? 0.f : rg;
+                    const float two = one * __shfl_up_sync(0xffffffffu, one, 1), four = two * __shfl_up_sync(0xffffffffu, two, 2);
+                    const float eight = four * __shfl_up_sync(0xffffffffu, four, 4);
+                    float to = one, from = __shfl_down_sync(0xffffffffu, one, 1);
+                    if (lane >= DS_C - 1) from = 1.f;
+#pragma unroll
+                    for (int off = 1; off < DS_C; off <<= 1) {
+                        const float x = __shfl_up_sync(0xffffffffu, to, off), y = __shfl_down_sync(0xffffffffu, from, off);
+                        if (lane >= off) to *= x;
+                        if (lane + off < DS_C) from *= y;
                     }
-                    ch.g[j] = d;
-                    ch.sg[j] = d * p.scale;
+                    if (lane < DS_C) {
+                        w.power[0][lane] = one; w.power[1][lane] = two; w.power[2][lane] = four; w.power[3][lane] = eight;
+                        w.beta[lane] = rb;
+                        w.left[lane] = from;
+                        ch.g[lane] = to;
+                        ch.sg[lane] = to * p.scale;
+                    }
                 }
+                fetch(c + DS_GROUPS);
+                group_sync(1 + group);
                 // warps 0, 1: k_j.k_i for 8 i each, 2, 3: q_j.k_i
-                const int pw = warp - 4, i8 = 8 * (pw & 1), fr = lane >> 2, fq = lane & 3;
                 float f[4];
                 product<D / 8>(f, ch.kq[pw < 2 ? 0 : DS_C], Ch::KP, 1, ch.kq[i8], 1, Ch::KP, 0, D / 8, lane);
-                PREP_SYNC();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = fr + 8 * (e >> 1), i = i8 + 2 * fq + (e & 1);
-                    if (pw < 2) w.a[j][i] = i < j ? w.beta[j] * w.decay[j][i] * f[e] : 0.f;
-                    else w.p[j][i] = i <= j ? p.scale * w.decay[j][i] * f[e] : 0.f;
+                for (int half = 0; half < 2; ++half) {
+                    const int j = fr + 8 * half, i = i8 + 2 * fq, many = max(j - i - 1, 0);
+                    float d1 = 1.f;      // D_j,i+1, from products of 1, 2, 4, 8 gates
+                    int at = j;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float x = w.power[k][at];
+                        const bool take = many >> k & 1;
+                        d1 *= take ? x : 1.f;
+                        at -= take ? 1 << k : 0;
+                    }
+                    const float next = w.power[0][i + 1];
+                    const float d0 = i < j ? d1 * next : 1.f, x0 = f[2 * half], x1 = f[2 * half + 1];
+                    if (pw < 2) {
+                        const float beta = w.beta[j];
+                        w.a[j][i] = i < j ? beta * d0 * x0 : 0.f;
+                        w.a[j][i + 1] = i + 1 < j ? beta * d1 * x1 : 0.f;
+                    } else {
+                        w.p[j][i] = i <= j ? p.scale * d0 * x0 : 0.f;
+                        w.p[j][i + 1] = i < j ? p.scale * d1 * x1 : 0.f;
+                    }
                 }
-                PREP_SYNC();
+                group_sync(1 + group);
                 // (I + A)^-1: two blocks of 8 by substitution (thread = column), then -c^-1 b a^-1 below them
                 if (u < 16) {
                     const int b = u & 8, col = u & 7;
+                    float4 a[8][2];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) {
+                        a[i][0] = *reinterpret_cast<const float4*>(&w.a[b + i][b]);
+                        a[i][1] = *reinterpret_cast<const float4*>(&w.a[b + i][b + 4]);
+                    }
                     float x[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float s0 = i == col ? 1.f : 0.f, s1 = 0.f;
-#pragma unroll
-                        for (int k = 0; k < i; ++k) {
-                            if (k & 1) s1 = fmaf(-w.a[b + i][b + k], x[k], s1);
-                            else s0 = fmaf(-w.a[b + i][b + k], x[k], s0);
-                        }
+                        if (i > 0) s0 = fmaf(-a[i][0].x, x[0], s0);
+                        if (i > 1) s1 = fmaf(-a[i][0].y, x[1], s1);
+                        if (i > 2) s0 = fmaf(-a[i][0].z, x[2], s0);
+                        if (i > 3) s1 = fmaf(-a[i][0].w, x[3], s1);
+                        if (i > 4) s0 = fmaf(-a[i][1].x, x[4], s0);
+                        if (i > 5) s1 = fmaf(-a[i][1].y, x[5], s1);
+                        if (i > 6) s0 = fmaf(-a[i][1].z, x[6], s0);
                         x[i] = s0 + s1;
                         w.t[b + i][b + col] = x[i];
                         if (b == 0) w.t[i][8 + col] = 0.f;
                     }
                 }
-                PREP_SYNC();
+                group_sync(1 + group);
                 if (u < 64) {
                     const int i = u >> 3, k = u & 7;
                     float s = 0.f;
@@ -156,7 +189,7 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
                     for (int e = 0; e < 8; ++e) s = fmaf(w.a[8 + i][e], w.t[e][k], s);
                     w.x[i][k] = s;
                 }
-                PREP_SYNC();
+                group_sync(1 + group);
                 if (u < 64) {
                     const int i = u >> 3, k = u & 7;
                     float s = 0.f;
@@ -164,15 +197,15 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
                     for (int e = 0; e < 8; ++e) s = fmaf(-w.t[8 + i][8 + e], w.x[e][k], s);
                     w.t[8 + i][k] = s;
                 }
-                PREP_SYNC();
+                group_sync(1 + group);
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {      // T = inverse diag(beta), and its rows weighted
                     const int s = u >> 3, t = 2 * (u & 7) + r;
                     const float x = w.t[s][t] * w.beta[t];
                     w.t[s][t] = x;
-                    w.wt[s][t] = x * w.decay[DS_C - 1][s];
+                    w.wt[s][t] = x * w.left[s];
                 }
-                PREP_SYNC();
+                group_sync(1 + group);
                 // Y transposed = (diag(D_15) T)^T K: D / 4 of its columns a warp; P T: 8 columns each of warps 0, 1
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
@@ -185,7 +218,7 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
                     put_fragment(&ch.pt[0][i8], Ch::TP, f, 1.f, lane);
                 }
             }
-            __syncthreads();      // chunk c is ready, chunk c - 1 has been walked
+            pass_arrive(5 + c % DS_BUFFERS);
         }
         return;
     }
@@ -212,8 +245,8 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
         for (int i = 0; i < TILES; ++i)
 #pragma unroll
             for (int k = 0; k < 2; ++k) put_fragment(&sh.s[16 * (warp + 4 * i)][8 * k], DeltaShared<D>::SP, s[i][k], 1.f, lane);
-        __syncthreads();      // chunk c is ready, and so is S
-        const Ch& ch = sh.chunk[c & 1];
+        pass_wait(5 + c % DS_BUFFERS);      // chunk c is ready, and so is S
+        const Ch& ch = sh.chunk[c % DS_BUFFERS];
         float f[4];
         product<D / 8>(f, ch.kq[warp < 2 ? 0 : DS_C], Ch::KP, 1, &sh.s[0][n0], DeltaShared<D>::SP, 1, 0, D / 8, lane);
         if (warp < 2) {
@@ -224,7 +257,7 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
             }
             put_fragment(&sh.r[0][n0], DeltaShared<D>::SP, f, 1.f, lane);
         }
-        WALK_SYNC();
+        group_sync(4);
         const float last = ch.g[DS_C - 1];
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
@@ -244,8 +277,8 @@ __global__ void __launch_bounds__(DS_THREADS) delta_simt_kernel(const DeltaParam
                 if (c * DS_C + t < len) o[(size_t)(c * DS_C + t) * p.H * D + col] = from_f32<T>(fmaf(ch.sg[t], f[e], d[e]));
             }
         }
+        if (c + DS_BUFFERS < chunks) pass_arrive(9 + c % DS_BUFFERS);
     }
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < TILES; ++i)
 #pragma unroll
