@@ -39,7 +39,7 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 __device__ __forceinline__ void tf32_terms(float x, uint32_t& hi, uint32_t& lo) {
-    hi = __float_as_uint(x) & 0xffffe000u;
+    hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;      // rounded: cut off, it would leave a low term of x's own sign, which the MMA cuts off towards zero again
     lo = __float_as_uint(x - __uint_as_float(hi));
 }
 // c = M[16 x 8 KT] B[8 KT x 8], both in shared memory: element (m, k) of M at m * mr + k * mk, (k, n) of B at k * bk + n * bn; steps of 8 from k_first up to

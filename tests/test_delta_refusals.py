@@ -31,6 +31,17 @@ def test_delta_prefill(b):
     assert b.dsla_delta_prefill_workspace_bytes(512, 1, 512, 4, 64, torch.bfloat16, impl="simt", dense_T=512) == 0
 
 
+def test_workspace_is_what_the_kernel_uses(b):
+    """A chunk of 64 tokens and a head take Y in two terms [d][64], P T [64][64], all bf16, and two gates per token; packed batches one chunk more per sequence."""
+    for d in (64, 128):
+        entry = 2 * d * 128 + 64 * 128 + 2 * 64 * 4
+        assert b.dsla_delta_prefill_workspace_bytes(4096, 1, 4096, 32, d, dense_T=4096) == 64 * 32 * entry
+        assert b.dsla_delta_prefill_workspace_bytes(3 * 65, 3, 65, 8, d, dense_T=65) == 3 * 2 * 8 * entry
+        assert b.dsla_delta_prefill_workspace_bytes(1000, 7, 900, 8, d) == (1000 // 64 + 7) * 8 * entry
+        assert b.dsla_delta_prefill_workspace_bytes(1000, 7, 900, 8, d, H_qk=2) == (1000 // 64 + 7) * 8 * entry
+    assert b.dsla_delta_prefill_workspace_bytes(0, 3, 0, 8, 128) == 0 and b.dsla_delta_prefill_workspace_bytes(1000, 7, 900, 8, 128, H_qk=3) == 0
+
+
 def test_delta_decode(b):
     a = b.dsla_delta_decode_args()
     a.B, a.H, a.H_qk, a.d_k, a.d_v = 1, 2, 2, 64, 64

@@ -340,3 +340,62 @@ def test_serving_loop(dtype):
         assert rel_err(y.double().cpu(), o) <= TOL_O[dtype]
     assert rel_err(final.double().cpu(), want_state) <= TOL_S
     assert torch.equal(st.tensor[1], final[2]) and torch.equal(st.tensor[0], final[0]) and not bool(st.tensor[2:].any())
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+@pytest.mark.parametrize("resume", [False, True])
+def test_more_heads_than_sms(impl, dtype, d, resume):
+    """So many (sequence, head) pairs that a CTA takes 64 columns."""
+    _check([70, 200, 1, 0, 129, 64], 40, 2, d, dtype, impl, seed=21, resume=resume, slots=[3, 5, 0, 1, 6, 2], extra_slots=1)
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+def test_bad_values_stay_in_their_sequence_with_many_heads(impl, dtype, d):
+    dsla = _dsla()
+    q, k, v, g, b = _draw(150, 96, 1, d, dtype, 3)
+    cu = torch.tensor([0, 50, 100, 150], dtype=torch.int32, device="cuda")
+    st, st2 = (dsla.dsla_state_alloc_n(3, 1, 96, d, d) for _ in range(2))
+    want = dsla.dsla_delta_prefill(q, k, v, g, b, st, cu_seqlens=cu, max_seqlen=50, impl=impl)
+    for x in (q, k, v, g, b):
+        x[50:100] = float("nan")
+    got = dsla.dsla_delta_prefill(q, k, v, g, b, st2, cu_seqlens=cu, max_seqlen=50, impl=impl)
+    for a, e, n in ((0, 50, 0), (100, 150, 2)):
+        assert torch.equal(want[a:e], got[a:e]) and torch.equal(st.tensor[n], st2.tensor[n])
+
+
+@both
+def test_many_short_sequences(impl, dtype, d):
+    """More sequences than are put in order of length, some of them empty."""
+    lens = [int(x) for x in torch.randint(0, 40, (140,), generator=torch.Generator().manual_seed(1))]
+    _check(lens, 2, 1, d, dtype, impl, seed=22)
+
+
+@both
+def test_rows_behind_the_last_sequence_are_left_alone(impl, dtype, d):
+    dsla = _dsla()
+    q, k, v, g, b = _draw(200, 2, 1, d, dtype, 6)
+    for x in (q, k, v, g, b):
+        x[130:] = float("nan")
+    cu = torch.tensor([0, 60, 130], dtype=torch.int32, device="cuda")
+    o = torch.full_like(v, 5.0)
+    st = dsla.dsla_state_alloc_n(2, 1, 2, d, d)
+    dsla.dsla_delta_prefill(q, k, v, g, b, st, o=o, cu_seqlens=cu, max_seqlen=70, impl=impl)
+    assert bool((o[130:] == 5).all()) and bool(torch.isfinite(o[:130]).all()) and bool(torch.isfinite(st.tensor).all())
+
+
+@pytest.mark.parametrize("impl", ["tensor", "simt"])
+def test_tokens_far_into_a_packed_batch(impl):
+    """Element offsets beyond 32 bits: a sequence of 150 tokens behind 540K rows that belong to none (cu_seqlens begins behind them)."""
+    dsla = _dsla()
+    H, d, far, n = 32, 128, 540_000, 150
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    tail = _draw(n, H, 1, d, BF, 8)
+    whole = [torch.zeros((far + n,) + x.shape[1:], dtype=x.dtype, device="cuda") for x in tail]
+    for x, y in zip(whole, tail):
+        x[far:] = y
+    st, small = (dsla.dsla_state_alloc_n(1, 1, H, d, d) for _ in range(2))
+    o = torch.zeros_like(whole[2])
+    got = dsla.dsla_delta_prefill(*whole, st, o=o, cu_seqlens=torch.tensor([far, far + n], dtype=torch.int32, device="cuda"), max_seqlen=n, impl=impl)
+    want = dsla.dsla_delta_prefill(*tail, small, impl=impl)
+    assert torch.equal(got[far:], want) and torch.equal(st.tensor, small.tensor) and not bool(got[:far].any())
