@@ -2,7 +2,8 @@
 //     y = w x r,   r = rsqrt(mean(x^2) + eps) | rsqrt(sum(x^2) + eps) | 1;      (a, b) -> (a cos f - b sin f, b cos f + a sin f)
 // A lane holds two pieces of four channels of a head, chosen so that the channels that turn with each other are its own: i and i + rot/2 (or the
 // neighbours 2i, 2i + 1), so only the sum of squares crosses lanes (with eight neighbouring channels to a lane the rotation took eight shuffles, and
-// the shuffles the time: 37 us for a 4K prompt).  A CTA takes the heads of one token: the rot/2 angles and their sines are computed once for all of them, while the
+// the shuffles the time: 37 us for 4096 tokens of 64 heads of 128 in bf16, now 28, 4.8 TB/s; fetching rounds ahead through shared memory, or several tokens a CTA, made it no
+// shorter).  A CTA takes the heads of one token: the rot/2 angles and their sines are computed once for all of them, while the
 // first heads are on their way.  An angle is a product in fp64, reduced to half turns there: at position 100,000 an fp32 product is off by
 // 4e-3 radians.  Bound by HBM: x read once, y written once.
 #include "dsla_internal.cuh"
@@ -37,7 +38,7 @@ template <> struct Four<__nv_bfloat16> {
 };
 
 template <int D, typename T, int NORM, bool INTERLEAVED>
-__global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_norm_rope_args p, int per) {
+__global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_norm_rope_args p) {
     constexpr int LANES = D / 8, HEADS = QN_THREADS / LANES;      // lanes per head, heads per CTA at a time
     constexpr int AHEAD = 4;                                      // rounds of heads whose loads are issued together
     __shared__ __align__(16) float scos[D / 2], ssin[D / 2];
@@ -45,7 +46,7 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
     const int rot = p.rot, half = rot / 2;
     const bool turns = lane < rot / 8;                            // this lane's channels turn
     const int at0 = !INTERLEAVED && turns ? 4 * lane : 8 * lane, at1 = !INTERLEAVED && turns ? half + 4 * lane : 8 * lane + 4;
-    const int begin = blockIdx.y * per, end = min(begin + per, p.H + p.H_k);      // heads of this CTA, q's first
+    const int end = p.H + p.H_k;                                  // heads, q's first
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Four<T> in[AHEAD][2];
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
             }
         }
     };
-    load(begin);
+    load(0);
     float wq[8], wk[8], cs[4], sn[4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -83,8 +84,8 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
             for (int i = 0; i < 4; ++i) { cs[i] = scos[4 * lane + i]; sn[i] = ssin[4 * lane + i]; }
         }
     }
-    for (int h0 = begin; h0 < end; h0 += AHEAD * HEADS) {
-        if (h0 > begin) load(h0);
+    for (int h0 = 0; h0 < end; h0 += AHEAD * HEADS) {
+        if (h0 > 0) load(h0);
 #pragma unroll
         for (int r = 0; r < AHEAD; ++r) {
             if (h0 + r * HEADS >= end) break;
@@ -125,30 +126,24 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
 }
 
 template <int D, typename T, int NORM>
-cudaError_t launch_order(const cudaLaunchConfig_t* cfg, const dsla_qk_norm_rope_args& a, int per) {
-    return a.interleaved ? cudaLaunchKernelEx(cfg, qk_norm_rope_kernel<D, T, NORM, true>, a, per)
-                         : cudaLaunchKernelEx(cfg, qk_norm_rope_kernel<D, T, NORM, false>, a, per);
+cudaError_t launch_order(const cudaLaunchConfig_t* cfg, const dsla_qk_norm_rope_args& a) {
+    return a.interleaved ? cudaLaunchKernelEx(cfg, qk_norm_rope_kernel<D, T, NORM, true>, a)
+                         : cudaLaunchKernelEx(cfg, qk_norm_rope_kernel<D, T, NORM, false>, a);
 }
 template <int D, typename T>
-cudaError_t launch_norm(const cudaLaunchConfig_t* cfg, const dsla_qk_norm_rope_args& a, int per) {
+cudaError_t launch_norm(const cudaLaunchConfig_t* cfg, const dsla_qk_norm_rope_args& a) {
     switch (a.norm) {
-        case DSLA_NORM_RMS: return launch_order<D, T, DSLA_NORM_RMS>(cfg, a, per);
-        case DSLA_NORM_L2: return launch_order<D, T, DSLA_NORM_L2>(cfg, a, per);
-        default: return launch_order<D, T, DSLA_NORM_NONE>(cfg, a, per);
+        case DSLA_NORM_RMS: return launch_order<D, T, DSLA_NORM_RMS>(cfg, a);
+        case DSLA_NORM_L2: return launch_order<D, T, DSLA_NORM_L2>(cfg, a);
+        default: return launch_order<D, T, DSLA_NORM_NONE>(cfg, a);
     }
 }
 
 }  // namespace
 
 dsla_status launch_qk_norm_rope(const dsla_qk_norm_rope_args* a, cudaStream_t s) {
-    const int total = a->H + a->H_k;
-    const int at_once = QN_THREADS / (a->d / 8);
-    const int per = total;
-    const int parts = (total + per - 1) / per;
-    (void)at_once;
-    if (parts > 65535) return DSLA_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a->T, (unsigned)parts);
+    cfg.gridDim = dim3((unsigned)a->T);
     cfg.blockDim = dim3(QN_THREADS);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -157,8 +152,8 @@ dsla_status launch_qk_norm_rope(const dsla_qk_norm_rope_args* a, cudaStream_t s)
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t rc;
-    if (a->d == 128) rc = a->dtype == DSLA_BF16 ? launch_norm<128, __nv_bfloat16>(&cfg, *a, per) : launch_norm<128, float>(&cfg, *a, per);
-    else rc = a->dtype == DSLA_BF16 ? launch_norm<64, __nv_bfloat16>(&cfg, *a, per) : launch_norm<64, float>(&cfg, *a, per);
+    if (a->d == 128) rc = a->dtype == DSLA_BF16 ? launch_norm<128, __nv_bfloat16>(&cfg, *a) : launch_norm<128, float>(&cfg, *a);
+    else rc = a->dtype == DSLA_BF16 ? launch_norm<64, __nv_bfloat16>(&cfg, *a) : launch_norm<64, float>(&cfg, *a);
     if (rc != cudaSuccess) return DSLA_ERR_CUDA;
     count_launch();
     return cudaGetLastError() == cudaSuccess ? DSLA_OK : DSLA_ERR_CUDA;
