@@ -312,15 +312,15 @@ dsla_status dsla_state_copy(dsla_state* st, const int32_t* src_slots, const int3
  * beta_t in [0, 1] (or beta |k|^2 <= 2) keep the recurrence from growing; it is not bounded otherwise, in any form.  H_qk heads of queries
  * and keys serve H = group * H_qk heads of values, gates and states: value head h reads head h / group.  (No counterpart in the paper.)
  *
- * Two kernels for prompts:
- *   SIMT   : the recurrence token by token on CUDA cores in fp32; every dtype and head size, no workspace.
- *   TENSOR : bf16 (heads of 64 or 128), chunks of 64 tokens on the tensor cores.  With G_j the product of the chunk's gates up to j and
- *            D_ji that of the gates i+1 .. j, the u of a chunk solve (I + tril(beta_j D_ji k_j.k_i, -1)) U = beta (V - G K S); the
- *            inverses of all chunks are computed first, in parallel, into the workspace, then each sequence walks its chunks.
- *            Everything that reaches a state is held in 16 bits or more of mantissa and summed in fp32 (states 3e-6 from the token-by-token ones).
+ * Prompts are taken in chunks.  With G_j the product of the chunk's gates up to j and D_ji that of the gates i+1 .. j, the u of a chunk solve
+ * (I + tril(beta_j D_ji k_j.k_i, -1)) U = beta (V - G K S).
+ *   SIMT   : chunks of 16 tokens in fp32 (products of two TF32 terms, 22 bits), every dtype and head size, no workspace.
+ *   TENSOR : bf16 (heads of 64 or 128), chunks of 64 tokens on the tensor cores: the inverses of all chunks are computed first, in parallel, into the
+ *            workspace, then each (sequence, head) walks its chunks.  Everything that reaches a state is held in 16 bits of mantissa or more and summed
+ *            in fp32 (states within 1e-5 of the token-by-token ones).
  *   AUTO   : TENSOR for bf16, else SIMT.
- * A call of impl TENSOR or AUTO is refused (DSLA_ERR_INVALID_ARG) without the workspace that dsla_delta_prefill_workspace_bytes() reports.
- * An infinity or NaN in a token reaches, with TENSOR, the outputs of its whole chunk of 64 tokens, never those of another sequence.
+ * A call that runs TENSOR is refused (DSLA_ERR_INVALID_ARG) without the workspace that dsla_delta_prefill_workspace_bytes() reports.
+ * An infinity or NaN in a token reaches, at most, the outputs of its whole chunk and all later ones of its sequence, never those of another sequence.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
     const void* q;              /* [T_total, H_qk, d_k] dtype, row-major, 16-byte aligned                     */
@@ -343,8 +343,8 @@ typedef struct {
 
 size_t dsla_delta_prefill_workspace_bytes(const dsla_delta_prefill_args* a);
 
-/* Writes o for every token and the final state of every sequence into its slot; sequences of length 0 as in dsla_prefill, and so are the
- * errors that only the device can see (dsla_state_last_error). */
+/* Writes o for every token and the final state of every sequence into its slot; sequences of length 0 as in dsla_prefill.  max_seqlen is an
+ * upper bound that only the checks read.  A wait that gave up is reported by dsla_state_last_error, as there. */
 dsla_status dsla_delta_prefill(const dsla_delta_prefill_args* a, dsla_state* st, void* cuda_stream);
 
 typedef struct {

@@ -4,6 +4,7 @@
 //     A = tril(beta_j D_ji k_j.k_i, -1),   T = (I + A)^-1 diag(beta),   P = scale tril(D_ji q_j.k_i),   Y = K^T diag(2^(L_63 - L)) T
 // a chunk is
 //     R = V - G K S,       O = scale G Q S + (P T) R,       S <- G_63 S + Y R .
+// (4096 tokens, 32 heads of 128: 142 us, the first kernel 50 of them; token by token 1714.)
 // Y and P T need no state: a first kernel computes them for all chunks at once (one CTA per chunk and head) into the workspace, a second one walks the
 // chunks of each sequence, two dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v).
 //
@@ -342,7 +343,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
     }
     __syncthreads();
     // T = inverse diag(beta) into tiles, then with its rows weighted; thread = 16 columns of a row
-    const int ts = tid >> 2, tc0 = 16 * (tid & 3);
+    const int ts = tid & 63, tc0 = 16 * (tid >> 6);      // (a warp's rows of one column group: no bank is asked twice)
     uint8_t* const t_at = work + PREP_T + ts * 128;
     uint32_t w[3][8];
     {
@@ -472,6 +473,10 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 //   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
+// Bound by shared memory and the chain: a chunk takes 2250 cycles, of which copies in (78 KB), operands of 20 MMAs (120 KB) and the rows' own accesses hold its port for about 1850;
+// with W = 64 3400 cycles, 2500 of them held, so half the CTAs of twice the width do more in all once there are enough of them (58K ragged tokens, 32 heads: 1.90 ms with
+// W = 32, 1.73 with W = 64; one sequence of 4096 tokens 143 and 182 us).  Slices of a sequence, the first kernel for one slice under the walk of the slice before, took
+// as long as one after the other (4096 tokens 151 us): both want that port.
 constexpr int WC = 16, ST = 2;      // columns of a thread; stages of loads
 
 template <int D_, int W_>
@@ -559,7 +564,7 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     const uint32_t tb = tmem_base;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (p.cu_seqlens && p.N > 1 && p.N <= 128) {      // the longest sequences first (58K tokens in 16 sequences of 1 to 8K: xx ms in the order given)
+    if (p.cu_seqlens && p.N > 1 && p.N <= 128) {      // the longest sequences first (58K tokens in 16 sequences of 1 to 8K: 1.55 ms in the order given, 1.47 so)
         if (tid < p.N) {
             const int mine = p.cu_seqlens[tid + 1] - p.cu_seqlens[tid];
             int rank = 0, from = p.cu_seqlens[0];
