@@ -113,7 +113,6 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
     volatile int* abortp = &abort_flag;
     const int h = blockIdx.x % p.H;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int n, t_begin, len, first;
     const int at = blockIdx.x / p.H;
     if (p.cu_seqlens) {      // the last sequence whose slots begin at or before this one
@@ -196,6 +195,8 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // The walk's CTAs take their tensor memory before they wait for this grid, so they may start only when every CTA here has its own.
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tb = tmem_base;
     if (warp == 0 && elect_one()) {
         WAIT(&full, 0);
@@ -833,6 +834,8 @@ dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cu
         cfg.dynamicSmemBytes = Prep<D>::SMEM;
         if (cudaLaunchKernelEx(&cfg, delta_chunk_kernel<D>, mk, mq, tp) != cudaSuccess) return DSLA_ERR_CUDA;
         count_launch();
+    } else {
+        cfg.numAttrs = 0;      // not ahead of whatever kernel comes before: it may still want tensor memory
     }
     const dsla_status rc = (long long)p.N * p.H * (D / 32) <= sm_count() ? launch_walk<D, 32>(cfg, mk, mq, mo, tp, a->T_total)
                                                                            : launch_walk<D, 64>(cfg, mk, mq, mo, tp, a->T_total);
