@@ -478,6 +478,9 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 // with W = 64 3400 cycles, 2500 of them held, so half the CTAs of twice the width do more in all once there are enough of them (58K ragged tokens, 32 heads: 1.90 ms with
 // W = 32, 1.73 with W = 64; one sequence of 4096 tokens 143 and 182 us).  Slices of a sequence, the first kernel for one slice under the walk of the slice before, took
 // as long as one after the other (4096 tokens 151 us): both want that port.
+// Where there are more (sequence, head, columns) than SMs, a CTA that is done takes over a block of the grid that has not started, two of them ahead: the next one's
+// loads run under the end of this one's, and barriers and tensor memory are set up once (64 sequences of 64 tokens, 32 heads of 128: 298 us with a CTA for
+// each, 242 so; of 512 tokens 990 and 900).
 constexpr int WC = 16, ST = 2;      // columns of a thread; stages of loads
 
 template <int D_, int W_>
@@ -527,23 +530,55 @@ __device__ __forceinline__ void put_split(uint8_t* tile, int lbo, int r, int par
     }
 }
 
+// What a CTA works on: one sequence, head and W columns.  `chunks` < 0: nothing any more.
+struct Item {
+    int t_begin, len, first, slot, h, column, chunks;
+    bool live;      // has a state to write
+};
+// Asks for the place in the grid of a CTA that has not started, which then never does.  By one thread; the answer, 16 bytes, arrives at the barrier.
+__device__ __forceinline__ void ask_for_next(void* to, uint64_t* bar) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(to)), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ int next_block(const void* from) {      // -1: all have started
+    int x;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t.reg .b32 a, b, c, d;\n\t"
+        "ld.shared.b128 r, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "mov.b32 a, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {a, b, c, d}, r;\n\t"
+        "mov.b32 %0, a;\n\t}"
+        : "=r"(x)
+        : "r"(smem_u32(from))
+        : "memory");
+    return x;
+}
+// Named barriers between the loading warp and all others: item `it` has been published, and read.  (Both sides get to each: their other waits are bounded.)
+template <int THREADS> __device__ __forceinline__ void item_wait(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
+template <int THREADS> __device__ __forceinline__ void item_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
+constexpr int PUBLISHED = 3, READ = 5;
+
 template <int D, int W>
 __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
                                                                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
     using L = Walk<D, W>;
     using In = Chunk<D>;
+    constexpr bool MORE = W > 32;      // slabs of 32 columns are for grids that fit on the device at once
     constexpr int SLABS = D / W, MMA_WARP = L::ROW_WARPS, LOAD_WARP = MMA_WARP + 1;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free;
+    __shared__ __align__(16) uint8_t answer[16];
+    __shared__ uint64_t answered;
+    __shared__ Item items[2];
+    __shared__ uint8_t order[128];
     __shared__ uint32_t tmem_base;
-    __shared__ int abort_flag, sequence;
+    __shared__ int abort_flag;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
     const DeltaParams& p = tp.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abortp = &abort_flag;
-    const int slab = blockIdx.x % SLABS, h = (blockIdx.x / SLABS) % p.H;
-    int n = blockIdx.x / (SLABS * p.H);
-
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
             mbar_init(&kq_full[i], 1);
@@ -551,6 +586,7 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
             mbar_init(&y_full[i], 1);
             mbar_init(&y_empty[i], 1 + L::ROW_WARPS / 2);      // the MMAs, and the warps that read the gates off the chain
         }
+        mbar_init(&answered, 1);
         mbar_init(&x_full, 1);
         mbar_init(&d_full, 1);
         mbar_init(&o_full, 1);
@@ -565,7 +601,8 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     const uint32_t tb = tmem_base;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (p.cu_seqlens && p.N > 1 && p.N <= 128) {      // the longest sequences first (58K tokens in 16 sequences of 1 to 8K: 1.55 ms in the order given, 1.47 so)
+    const bool sorted = p.cu_seqlens && p.N > 1 && p.N <= 128;
+    if (sorted) {      // the longest sequences first (58K tokens in 16 sequences of 1 to 8K: 1.55 ms in the order given, 1.47 so)
         if (tid < p.N) {
             const int mine = p.cu_seqlens[tid + 1] - p.cu_seqlens[tid];
             int rank = 0, from = p.cu_seqlens[0];
@@ -574,98 +611,125 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
                 rank += other > mine || (other == mine && k < tid);
                 from = to;
             }
-            if (rank == n) sequence = tid;
+            order[rank] = (uint8_t)tid;
         }
         __syncthreads();
-        n = sequence;
     }
-    int t_begin, len, first;
-    find_sequence(tp, n, t_begin, len, first);
-    const int slot = p.slots ? p.slots[n] : n;
-    const bool work = slot >= 0 && slot < p.num_slots && (len > 0 || !p.use_initial_state);
-    const int nc = work ? (len + DC - 1) / DC : 0;
 
     if (warp == LOAD_WARP) {
-        if (lane == 0 && nc > 0) {
+        if (lane == 0) {
             prefetch_tensormap(&map_k);
             prefetch_tensormap(&map_q);
             prefetch_tensormap(&map_v);
             prefetch_tensormap(&map_o);
-            const int hq = h / p.group;
-            for (int c = 0; c < nc && !*abortp; ++c) {
-                const int st = c % ST;
-                if (c >= ST) WAIT(&kq_empty[st], (c / ST - 1) & 1);
-                uint8_t* to = sm + st * L::KQ;
-                mbar_arrive_expect_tx(&kq_full[st], L::KQ);
-                for (int half = 0; half < D / 64; ++half) {
-                    tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[st], 0, t_begin + c * DC, half, hq);
-                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[st], 0, t_begin + c * DC, half, hq);
+        }
+        int block = blockIdx.x, cc = 0;      // cc: chunks of all items so far
+        for (int it = 0;; ++it) {
+            Item x{};
+            x.chunks = -1;
+            if (block >= 0) {
+                if (MORE && lane == 0) ask_for_next(answer, &answered);
+                const int place = block / (SLABS * p.H), n = sorted ? order[place] : place;
+                find_sequence(tp, n, x.t_begin, x.len, x.first);
+                x.slot = p.slots ? p.slots[n] : n;
+                x.h = (block / SLABS) % p.H;
+                x.column = block % SLABS * W;
+                x.live = x.slot >= 0 && x.slot < p.num_slots && (x.len > 0 || !p.use_initial_state);
+                x.chunks = x.live ? (x.len + DC - 1) / DC : 0;
+            }
+            if (it >= 2) item_wait<L::THREADS>(READ + (it & 1));
+            if (lane == 0) items[it & 1] = x;
+            __syncwarp();
+            item_arrive<L::THREADS>(PUBLISHED + (it & 1));
+            if (block < 0) break;
+            if (x.live && p.use_initial_state)      // rows of the state, on their way before they are asked for
+                for (int i = lane; i < D; i += 32)
+                    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.state + (((size_t)x.slot * p.H + x.h) * D + i) * D + x.column), "n"(W * 4) : "memory");
+            if (lane == 0) {
+                const int hq = x.h / p.group;
+                for (int c = 0; c < x.chunks && !*abortp; ++c, ++cc) {
+                    const int st = cc % ST;
+                    if (cc >= ST) WAIT(&kq_empty[st], (cc / ST - 1) & 1);
+                    uint8_t* to = sm + st * L::KQ;
+                    mbar_arrive_expect_tx(&kq_full[st], L::KQ);
+                    for (int half = 0; half < D / 64; ++half) {
+                        tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[st], 0, x.t_begin + c * DC, half, hq);
+                        tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[st], 0, x.t_begin + c * DC, half, hq);
+                    }
+                    if (cc >= ST) WAIT(&y_empty[st], (cc / ST - 1) & 1);
+                    to = sm + L::OFF_Y + st * L::Y_STAGE;
+                    mbar_arrive_expect_tx(&y_full[st], L::Y_BYTES);
+                    bulk_load(to, tp.ws + ((size_t)(x.first + c) * p.H + x.h) * In::BYTES, In::BYTES, &y_full[st]);
+                    tma_load_3d(to + L::V, &map_v, &y_full[st], x.column, x.h, x.t_begin + c * DC);
                 }
-                if (c >= ST) WAIT(&y_empty[st], (c / ST - 1) & 1);
-                to = sm + L::OFF_Y + st * L::Y_STAGE;
-                mbar_arrive_expect_tx(&y_full[st], L::Y_BYTES);
-                bulk_load(to, tp.ws + ((size_t)(first + c) * p.H + h) * In::BYTES, In::BYTES, &y_full[st]);
-                tma_load_3d(to + L::V, &map_v, &y_full[st], slab * W, h, t_begin + c * DC);
+            }
+            __syncwarp();
+            block = -1;
+            if (MORE) {
+                WAIT(&answered, it & 1);
+                block = __shfl_sync(0xffffffffu, *abortp ? -1 : next_block(answer), 0);
             }
         }
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
         constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1);
-        for (int c = 0; c < nc; ++c) {
-            const int st = c % ST;
-            const uint32_t kq = base + st * L::KQ, y = base + L::OFF_Y + st * L::Y_STAGE;
-            WAIT(&kq_full[st], (c / ST) & 1);
-            rows_wait<1, L::ROW_WARPS>();
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                    mma_ss(tb + L::COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, L::S_LBO, 1024), ID, kk ? 1u : 0u);
-                tc_commit(&x_full);
-                tc_commit(&kq_empty[st]);
-            }
+        int c = 0;      // chunks of all items
+        for (int it = 0;; ++it) {
+            item_wait<L::THREADS>(PUBLISHED + (it & 1));
+            const int chunks = items[it & 1].chunks;
             __syncwarp();
-            WAIT(&y_full[st], (c / ST) & 1);
-            if (c > 0) WAIT(&o_free, (c - 1) & 1);
-            rows_wait<2, L::ROW_WARPS / 2>();
-            tc_fence_after();
-            if (elect_one()) {
+            if (chunks < 0) break;
+            item_arrive<L::THREADS>(READ + (it & 1));
+            for (const int end = c + chunks; c < end; ++c) {
+                const int st = c % ST;
+                const uint32_t kq = base + st * L::KQ, y = base + L::OFF_Y + st * L::Y_STAGE;
+                WAIT(&kq_full[st], (c / ST) & 1);
+                rows_wait<1, L::ROW_WARPS>();
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 1; k >= 0; --k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        mma_ss(tb + L::COL_X, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), smem_desc_sw128(s_at + kk * 2048, L::S_LBO, 1024), ID, kk ? 1u : 0u);
+                    tc_commit(&x_full);
+                    tc_commit(&kq_empty[st]);
+                }
+                __syncwarp();
+                WAIT(&y_full[st], (c / ST) & 1);
+                if (c > 0) WAIT(&o_free, (c - 1) & 1);
+                rows_wait<2, L::ROW_WARPS / 2>();
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < DC / 16; ++kk)
-                        mma_ss(tb + L::COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, !k || kk ? 1u : 0u);
-                tc_commit(&d_full);
+                    for (int k = 1; k >= 0; --k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
 #pragma unroll
-                for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
-                    mma_ss(tb + L::COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, kk ? 1u : 0u);
-                tc_commit(&o_full);
-                tc_commit(&y_empty[st]);
+                        for (int kk = 0; kk < DC / 16; ++kk)
+                            mma_ss(tb + L::COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, !k || kk ? 1u : 0u);
+                    tc_commit(&d_full);
+#pragma unroll
+                    for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
+                        mma_ss(tb + L::COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, kk ? 1u : 0u);
+                    tc_commit(&o_full);
+                    tc_commit(&y_empty[st]);
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
-    } else if (work) {
+    } else {
         const int quad = warp & 3, row = 32 * quad + lane;      // lane of TMEM: d_k of the state; token (quadrants 0, 1: of R, 2, 3: of the outputs)
         const int part = warp >> 2;                             // which 16 of the W columns
         const uint32_t lane_addr = tb + ((uint32_t)(32 * quad) << 16) + WC * part;
         const bool has_state = row < D, makes_r = quad < 2;
         const int j = row & 63;
-        float* S = p.state + (((size_t)slot * p.H + h) * D + row) * D + slab * W + WC * part;
         uint64_t s[WC / 2], y[WC / 2];
 #pragma unroll
-        for (int i = 0; i < WC; i += 4) {
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (has_state && p.use_initial_state) x = *reinterpret_cast<const float4*>(S + i);
-            s[i / 2] = pair(x.x, x.y);
-            s[i / 2 + 1] = pair(x.z, x.w);
-            y[i / 2] = y[i / 2 + 1] = 0;
-        }
-        // The outputs of chunk c (quadrants 2, 3): y, scaled, and P T R.  Whole rows of 32 tokens leave by a TMA store of this warp; the stores of a ragged end
+        for (int i = 0; i < WC / 2; ++i) y[i] = 0;
+        int cc = 0;                                             // chunks of all items so far
+        // The outputs of chunk c (quadrants 2, 3), the latest of all: y, scaled, and P T R.  Whole rows of 32 tokens leave by a TMA store of this warp; the stores of a ragged end
         // come from the registers.
         uint8_t* o_tile = sm + L::OFF_O + ((quad & 1) * L::PARTS + part) * 1024;
-        auto outputs = [&](int c) {
+        auto outputs = [&](const Item& x, int c) {
             uint32_t a[WC], b[WC];
-            WAIT_HOT(&o_full, c & 1);
+            WAIT_HOT(&o_full, (cc - 1) & 1);
             tc_fence_after();
             tmem_ld16(lane_addr + L::COL_O, a);
             tmem_ld16(lane_addr + L::COL_O + W, b);
@@ -673,97 +737,112 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&o_free);
-            uint32_t x[WC / 2];
+            uint32_t z[WC / 2];
 #pragma unroll
             for (int i = 0; i < WC / 2; ++i) {
-                const float2 z = unpair(add2(y[i], add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1]))));
-                x[i] = pack_bf16(z.x, z.y);
+                const float2 u = unpair(add2(y[i], add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1]))));
+                z[i] = pack_bf16(u.x, u.y);
             }
             const int t0 = c * DC + 32 * (quad & 1);      // this warp's first token
-            if (t0 + 32 <= len) {
+            if (t0 + 32 <= x.len) {
                 if (lane == 0) bulk_wait_read();
                 __syncwarp();
-                *reinterpret_cast<uint4*>(o_tile + lane * 32) = make_uint4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<uint4*>(o_tile + lane * 32 + 16) = make_uint4(x[4], x[5], x[6], x[7]);
+                *reinterpret_cast<uint4*>(o_tile + lane * 32) = make_uint4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<uint4*>(o_tile + lane * 32 + 16) = make_uint4(z[4], z[5], z[6], z[7]);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    tma_store_3d(&map_o, o_tile, slab * W + WC * part, h, t_begin + t0);
+                    tma_store_3d(&map_o, o_tile, x.column + WC * part, x.h, x.t_begin + t0);
                     bulk_commit();
                 }
-            } else if (t0 + lane < len) {
-                uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(t_begin + t0 + lane) * p.H + h) * D + slab * W + WC * part);
-                to[0] = make_uint4(x[0], x[1], x[2], x[3]);
-                to[1] = make_uint4(x[4], x[5], x[6], x[7]);
+            } else if (t0 + lane < x.len) {
+                uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(x.t_begin + t0 + lane) * p.H + x.h) * D + x.column + WC * part);
+                to[0] = make_uint4(z[0], z[1], z[2], z[3]);
+                to[1] = make_uint4(z[4], z[5], z[6], z[7]);
             }
         };
-        for (int c = 0; c < nc; ++c) {
-            const int st = c % ST, live = min(DC, len - c * DC);
-            const uint8_t* stage = sm + L::OFF_Y + st * L::Y_STAGE;
-            const float* meta = reinterpret_cast<const float*>(stage + In::META);
-            uint32_t a[WC], b[WC];
-            float last;
-            if (has_state) put_split<W>(sm + L::OFF_S, L::S_LBO, row, part, s);
-            fence_proxy_async_smem();
-            tc_fence_before();
-            rows_arrive<1, L::ROW_WARPS>();
-            if (makes_r) {
-                WAIT_HOT(&y_full[st], (c / ST) & 1);
-                last = meta[2 * DC - 1];
-                const float G = -meta[DC + j];
-                uint4 vr[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)      // rows of 64 or 128 bytes, swizzled
-                    vr[i] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + (((2 * part + i) ^ (W == 32 ? (j >> 1) & 3 : j & 7)) << 4));
-                WAIT_HOT(&x_full, c & 1);
-                tc_fence_after();
-                tmem_ld16(lane_addr + L::COL_X, a);
-                tmem_ld16(lane_addr + L::COL_X + W, b);
-                tc_wait_ld();
-                uint64_t r[WC / 2];
-#pragma unroll
-                for (int i = 0; i < WC / 2; ++i) {
-                    const uint32_t word = reinterpret_cast<const uint32_t*>(vr)[i];
-                    r[i] = fma2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])), pair(word << 16, word & 0xffff0000u));
-                }
-                if (j >= live) {      // a token behind the sequence's end, whatever it holds
-#pragma unroll
-                    for (int i = 0; i < WC / 2; ++i) r[i] = 0;
-                }
-                put_split<W>(sm + L::OFF_R, L::R_LBO, j, part, r);
-                fence_proxy_async_smem();
-                tc_fence_before();
-                rows_arrive<2, L::ROW_WARPS / 2>();
-            } else {
-                if (c > 0) outputs(c - 1);
-                WAIT_HOT(&y_full[st], (c / ST) & 1);
-                last = meta[2 * DC - 1];
-                const float G = meta[j];
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&y_empty[st]);
-                WAIT_HOT(&x_full, c & 1);
-                tc_fence_after();
-                tmem_ld16(lane_addr + L::COL_X, a);
-                tmem_ld16(lane_addr + L::COL_X + W, b);
-                tc_wait_ld();
-#pragma unroll
-                for (int i = 0; i < WC / 2; ++i) y[i] = mul2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
-            }
-            WAIT_HOT(&d_full, c & 1);
-            tc_fence_after();
-            tmem_ld16(lane_addr + L::COL_D, a);
-            tmem_ld16(lane_addr + L::COL_D + W, b);
-            tc_wait_ld();
-            const uint64_t keep = pair(last, last);
-#pragma unroll
-            for (int i = 0; i < WC / 2; ++i) s[i] = fma2(keep, s[i], add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
-        }
-        if (!makes_r && nc > 0) outputs(nc - 1);
-        if (has_state) {
+        for (int it = 0;; ++it) {
+            item_wait<L::THREADS>(PUBLISHED + (it & 1));
+            const Item x = items[it & 1];
+            __syncwarp();
+            if (x.chunks < 0) break;
+            item_arrive<L::THREADS>(READ + (it & 1));
+            float* S = p.state + (((size_t)x.slot * p.H + x.h) * D + row) * D + x.column + WC * part;
 #pragma unroll
             for (int i = 0; i < WC; i += 4) {
-                const float2 x = unpair(s[i / 2]), z = unpair(s[i / 2 + 1]);
-                *reinterpret_cast<float4*>(S + i) = make_float4(x.x, x.y, z.x, z.y);
+                float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (has_state && x.live && p.use_initial_state) z = *reinterpret_cast<const float4*>(S + i);
+                s[i / 2] = pair(z.x, z.y);
+                s[i / 2 + 1] = pair(z.z, z.w);
+            }
+            for (int c = 0; c < x.chunks; ++c, ++cc) {
+                const int st = cc % ST, live = min(DC, x.len - c * DC);
+                const uint8_t* stage = sm + L::OFF_Y + st * L::Y_STAGE;
+                const float* meta = reinterpret_cast<const float*>(stage + In::META);
+                uint32_t a[WC], b[WC];
+                float last;
+                if (has_state) put_split<W>(sm + L::OFF_S, L::S_LBO, row, part, s);
+                fence_proxy_async_smem();
+                tc_fence_before();
+                rows_arrive<1, L::ROW_WARPS>();
+                if (makes_r) {
+                    WAIT_HOT(&y_full[st], (cc / ST) & 1);
+                    last = meta[2 * DC - 1];
+                    const float G = -meta[DC + j];
+                    uint4 vr[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)      // rows of 64 or 128 bytes, swizzled
+                        vr[i] = *reinterpret_cast<const uint4*>(stage + L::V + j * (W * 2) + (((2 * part + i) ^ (W == 32 ? (j >> 1) & 3 : j & 7)) << 4));
+                    WAIT_HOT(&x_full, cc & 1);
+                    tc_fence_after();
+                    tmem_ld16(lane_addr + L::COL_X, a);
+                    tmem_ld16(lane_addr + L::COL_X + W, b);
+                    tc_wait_ld();
+                    uint64_t r[WC / 2];
+#pragma unroll
+                    for (int i = 0; i < WC / 2; ++i) {
+                        const uint32_t word = reinterpret_cast<const uint32_t*>(vr)[i];
+                        r[i] = fma2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])), pair(word << 16, word & 0xffff0000u));
+                    }
+                    if (j >= live) {      // a token behind the sequence's end, whatever it holds
+#pragma unroll
+                        for (int i = 0; i < WC / 2; ++i) r[i] = 0;
+                    }
+                    put_split<W>(sm + L::OFF_R, L::R_LBO, j, part, r);
+                    fence_proxy_async_smem();
+                    tc_fence_before();
+                    rows_arrive<2, L::ROW_WARPS / 2>();
+                } else {
+                    if (c > 0) outputs(x, c - 1);
+                    WAIT_HOT(&y_full[st], (cc / ST) & 1);
+                    last = meta[2 * DC - 1];
+                    const float G = meta[j];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&y_empty[st]);
+                    WAIT_HOT(&x_full, cc & 1);
+                    tc_fence_after();
+                    tmem_ld16(lane_addr + L::COL_X, a);
+                    tmem_ld16(lane_addr + L::COL_X + W, b);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < WC / 2; ++i) y[i] = mul2(pair(G, G), add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
+                }
+                WAIT_HOT(&d_full, cc & 1);
+                tc_fence_after();
+                tmem_ld16(lane_addr + L::COL_D, a);
+                tmem_ld16(lane_addr + L::COL_D + W, b);
+                tc_wait_ld();
+                const uint64_t keep = pair(last, last);
+#pragma unroll
+                for (int i = 0; i < WC / 2; ++i) s[i] = fma2(keep, s[i], add2(pair(a[2 * i], a[2 * i + 1]), pair(b[2 * i], b[2 * i + 1])));
+            }
+            if (!makes_r && x.chunks > 0) outputs(x, x.chunks - 1);
+            if (has_state && x.live) {
+#pragma unroll
+                for (int i = 0; i < WC; i += 4) {
+                    const float2 u = unpair(s[i / 2]), w = unpair(s[i / 2 + 1]);
+                    *reinterpret_cast<float4*>(S + i) = make_float4(u.x, u.y, w.x, w.y);
+                }
             }
         }
         if (lane == 0) bulk_wait_read();
