@@ -399,3 +399,59 @@ def test_tokens_far_into_a_packed_batch(impl):
     got = dsla.dsla_delta_prefill(*whole, st, o=o, cu_seqlens=torch.tensor([far, far + n], dtype=torch.int32, device="cuda"), max_seqlen=n, impl=impl)
     want = dsla.dsla_delta_prefill(*tail, small, impl=impl)
     assert torch.equal(got[far:], want) and torch.equal(st.tensor, small.tensor) and not bool(got[:far].any())
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+@pytest.mark.parametrize("resume", [False, True])
+def test_many_blocks_a_cta(impl, dtype, d, resume):
+    """Several times more (sequence, head, 64 columns) than SMs, of lengths from none to some chunks, in slots out of order."""
+    lens = [1, 0, 130, 64, 3, 0, 65, 1, 1, 192, 0, 17, 128, 2, 63, 1]
+    _check(lens, 48, 3, d, dtype, impl, seed=23, resume=resume, slots=[(7 * i + 3) % 17 for i in range(16)])
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+def test_many_blocks_on_two_streams_and_in_graphs(impl, dtype, d):
+    """Two such calls at once on two streams, a store and a workspace each, then both from captured graphs: the same bits as one after the other."""
+    dsla = _dsla()
+    H, lens = 40, [70, 1, 0, 129, 5, 64, 200, 1, 33]
+    cu = torch.tensor([0] + list(np.cumsum(lens)), dtype=torch.int32, device="cuda")
+    kw = dict(cu_seqlens=cu, max_seqlen=200, impl=impl, use_initial_state=True)
+    sets = [_draw(sum(lens), H, 1, d, dtype, s) for s in (3, 4)]
+    stores = [dsla.dsla_state_alloc_n(len(lens), 1, H, d, d) for _ in sets]
+    want = []
+    for x, st in zip(sets, stores):
+        st.tensor.fill_(0.25)
+        want.append((dsla.dsla_delta_prefill(*x, st, **kw), st.tensor.clone()))
+    need = dsla.dsla_delta_prefill_workspace_bytes(sum(lens), len(lens), 200, H, d, dtype, impl=impl)
+    spaces = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in sets]
+    outs = [torch.empty_like(x[2]) for x in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+
+    def check(run):
+        for st, o in zip(stores, outs):
+            st.tensor.fill_(0.25)
+            o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        run()
+        torch.cuda.synchronize()
+        for (o, S), y, st in zip(want, outs, stores):
+            assert dsla.dsla_state_last_error(st) == dsla.DSLA_OK and torch.equal(o, y) and torch.equal(S, st.tensor)
+
+    def eager():
+        for x, st, o, ws, s in zip(sets, stores, outs, spaces, streams):
+            dsla.dsla_delta_prefill(*x, st, o=o, workspace=ws, stream=s, **kw)
+
+    graphs = []
+    for x, st, o, ws in zip(sets, stores, outs, spaces):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            dsla.dsla_delta_prefill(*x, st, o=o, workspace=ws, **kw)
+        graphs.append(gr)
+
+    def replayed():
+        for gr, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                gr.replay()
+
+    for run in (eager, replayed, eager, replayed):
+        check(run)
