@@ -2,11 +2,11 @@
 //     y = w x r,   r = rsqrt(mean(x^2) + eps) | rsqrt(sum(x^2) + eps) | 1;      (a, b) -> (a cos f - b sin f, b cos f + a sin f)
 // A lane holds two pieces of four channels of a head, chosen so that the channels that turn with each other are its own: i and i + rot/2 (or the
 // neighbours 2i, 2i + 1), so only the sum of squares crosses lanes (with eight neighbouring channels to a lane the rotation took eight shuffles, and
-// the shuffles the time: 37 us for 4096 tokens of 64 heads of 128 in bf16, now 28, 4.8 TB/s; fetching rounds ahead through shared memory, or several tokens a CTA, made it no
-// shorter).  A CTA takes the heads of one token: the rot/2 angles and their sines are computed once for all of them, while the
+// the shuffles the time: 37 us for 4096 tokens of 64 heads of 128 in bf16, now 27, 4.9 TB/s; fetching rounds ahead through shared memory, several tokens a CTA, or more CTAs an SM
+// made it no shorter).  A CTA takes the heads of one token: the rot/2 angles and their sines are computed once for all of them, while the
 // first heads are on their way.  An angle is a product in fp64, reduced to half turns there: at position 100,000 an fp32 product is off by
 // 4e-3 radians.  Bound by HBM: x read once, y written once.
-#include "dsla_internal.cuh"
+#include "dsla_delta.cuh"
 
 namespace dsla {
 
@@ -14,25 +14,30 @@ namespace {
 
 constexpr int QN_THREADS = 256;
 
-// Four neighbouring channels.
+// A lane's eight channels as pairs of fp32: u the first of those that turn with each other, v the second.  They come from two pieces of four
+// neighbours: piece 0 and 1, or, interleaved, the even and the odd channels of both.
+struct Eight { uint64_t u[2], v[2]; };
 template <typename T> struct Four;
 template <> struct Four<float> {
     float4 a;
     __device__ __forceinline__ void zero() { a = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); }
-    __device__ __forceinline__ void get(float* x) const { x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; }
-    static __device__ __forceinline__ void store(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+    __device__ __forceinline__ uint64_t first() const { return pair(a.x, a.y); }
+    __device__ __forceinline__ uint64_t second() const { return pair(a.z, a.w); }
+    __device__ __forceinline__ uint64_t even() const { return pair(a.x, a.z); }
+    __device__ __forceinline__ uint64_t odd() const { return pair(a.y, a.w); }
+    static __device__ __forceinline__ void store(float* p, float x, float y, float z, float w) { *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w); }
 };
 template <> struct Four<__nv_bfloat16> {
     uint2 a;
     __device__ __forceinline__ void zero() { a = make_uint2(0u, 0u); }
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint2*>(p); }
-    __device__ __forceinline__ void get(float* x) const {
-        x[0] = __uint_as_float(a.x << 16); x[1] = __uint_as_float(a.x & 0xffff0000u);
-        x[2] = __uint_as_float(a.y << 16); x[3] = __uint_as_float(a.y & 0xffff0000u);
-    }
-    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* x) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
+    __device__ __forceinline__ uint64_t first() const { return pair(a.x << 16, a.x & 0xffff0000u); }
+    __device__ __forceinline__ uint64_t second() const { return pair(a.y << 16, a.y & 0xffff0000u); }
+    __device__ __forceinline__ uint64_t even() const { return pair(a.x << 16, a.y << 16); }
+    __device__ __forceinline__ uint64_t odd() const { return pair(a.x & 0xffff0000u, a.y & 0xffff0000u); }
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, float x, float y, float z, float w) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(x, y), hi = __floats2bfloat162_rn(z, w);
         *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
     }
 };
@@ -42,6 +47,7 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
     constexpr int LANES = D / 8, HEADS = QN_THREADS / LANES;      // lanes per head, heads per CTA at a time
     constexpr int AHEAD = 4;                                      // rounds of heads whose loads are issued together
     __shared__ __align__(16) float scos[D / 2], ssin[D / 2];
+    __shared__ float4 weight[2][2][LANES];                        // of q and k: u's and v's of each lane
     const int t = blockIdx.x, tid = threadIdx.x, lane = tid % LANES;
     const int rot = p.rot, half = rot / 2;
     const bool turns = lane < rot / 8;                            // this lane's channels turn
@@ -66,22 +72,30 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
         }
     };
     load(0);
-    float wq[8], wk[8], cs[4], sn[4];
+    if (tid < 4 * LANES) {
+        const int of = tid / (2 * LANES), part = tid / LANES & 1;
+        const float* w = of ? p.k_weight : p.q_weight;
+        float x[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int at = (i < 4 ? at0 : at1) + (i & 3);
-        wq[i] = p.q_weight ? __ldg(p.q_weight + at) : 1.f;
-        wk[i] = p.k_weight ? __ldg(p.k_weight + at) : 1.f;
-    }
-    if (rot > 0) {
-        if (tid < half) {
-            const double turned = (double)p.positions[t] * (double)p.inv_freq[tid] * 0.31830988618379067154;      // half turns
-            sincospif((float)(turned - 2.0 * rint(0.5 * turned)), &ssin[tid], &scos[tid]);
+        for (int i = 0; i < 4; ++i) {
+            const int at = INTERLEAVED ? 8 * lane + 2 * i + part : (part ? at1 : at0) + i;
+            x[i] = w ? __ldg(w + at) : 1.f;
         }
-        __syncthreads();
-        if (turns) {
+        weight[of][part][lane] = make_float4(x[0], x[1], x[2], x[3]);
+    }
+    if (tid < half) {
+        const double turned = (double)p.positions[t] * (double)p.inv_freq[tid] * 0.31830988618379067154;      // half turns
+        sincospif((float)(turned - 2.0 * rint(0.5 * turned)), &ssin[tid], &scos[tid]);
+    }
+    __syncthreads();
+    uint64_t cs[2] = {0, 0}, sn[2] = {0, 0}, minus[2] = {0, 0};
+    if (turns) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { cs[i] = scos[4 * lane + i]; sn[i] = ssin[4 * lane + i]; }
+        for (int i = 0; i < 2; ++i) {
+            const float2 c = *reinterpret_cast<const float2*>(scos + 4 * lane + 2 * i), s = *reinterpret_cast<const float2*>(ssin + 4 * lane + 2 * i);
+            cs[i] = pair(c.x, c.y);
+            sn[i] = pair(s.x, s.y);
+            minus[i] = pair(-s.x, -s.y);
         }
     }
     for (int h0 = 0; h0 < end; h0 += AHEAD * HEADS) {
@@ -91,35 +105,44 @@ __global__ void __launch_bounds__(QN_THREADS) qk_norm_rope_kernel(const dsla_qk_
             if (h0 + r * HEADS >= end) break;
             const int h = h0 + r * HEADS + tid / LANES;      // heads behind the last: zeros, not stored; the shuffles run in all lanes
             const bool is_k = h >= p.H;
-            float x[8];
-            in[r][0].get(x);
-            in[r][1].get(x + 4);
+            const Four<T>&c0 = in[r][0], &c1 = in[r][1];
+            Eight x;
+            if (INTERLEAVED) x = {{c0.even(), c1.even()}, {c0.odd(), c1.odd()}};
+            else x = {{c0.first(), c0.second()}, {c1.first(), c1.second()}};
+            const float4 wu = weight[is_k][0][lane], wv = weight[is_k][1][lane];
             if (NORM != DSLA_NORM_NONE) {
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+                const float2 s = unpair(add2(fma2(x.u[0], x.u[0], mul2(x.u[1], x.u[1])), fma2(x.v[0], x.v[0], mul2(x.v[1], x.v[1]))));
+                float sum = s.x + s.y;
 #pragma unroll
                 for (int m = 1; m < LANES; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
                 const float f = rsqrtf((NORM == DSLA_NORM_RMS ? sum * (1.f / D) : sum) + p.eps);
+                const uint64_t ff = pair(f, f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] *= f;
+                for (int i = 0; i < 2; ++i) { x.u[i] = mul2(x.u[i], ff); x.v[i] = mul2(x.v[i], ff); }
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= is_k ? wk[i] : wq[i];
+            x.u[0] = mul2(x.u[0], pair(wu.x, wu.y));
+            x.u[1] = mul2(x.u[1], pair(wu.z, wu.w));
+            x.v[0] = mul2(x.v[0], pair(wv.x, wv.y));
+            x.v[1] = mul2(x.v[1], pair(wv.z, wv.w));
             if (turns) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int a = INTERLEAVED ? 2 * i : i, b = INTERLEAVED ? 2 * i + 1 : i + 4;
-                    const float u = x[a], v = x[b];
-                    x[a] = fmaf(u, cs[i], -(v * sn[i]));
-                    x[b] = fmaf(v, cs[i], u * sn[i]);
+                for (int i = 0; i < 2; ++i) {
+                    const uint64_t u = x.u[i], v = x.v[i];
+                    x.u[i] = fma2(u, cs[i], mul2(v, minus[i]));
+                    x.v[i] = fma2(v, cs[i], mul2(u, sn[i]));
                 }
             }
             if (h < end) {
                 T* dst = is_k ? reinterpret_cast<T*>(p.k_out) + (size_t)t * p.k_out_stride + (size_t)(h - p.H) * D
                               : reinterpret_cast<T*>(p.q_out) + (size_t)t * p.q_out_stride + (size_t)h * D;
-                Four<T>::store(dst + at0, x);
-                Four<T>::store(dst + at1, x + 4);
+                const float2 u0 = unpair(x.u[0]), u1 = unpair(x.u[1]), v0 = unpair(x.v[0]), v1 = unpair(x.v[1]);
+                if (INTERLEAVED) {
+                    Four<T>::store(dst + at0, u0.x, v0.x, u0.y, v0.y);
+                    Four<T>::store(dst + at1, u1.x, v1.x, u1.y, v1.y);
+                } else {
+                    Four<T>::store(dst + at0, u0.x, u0.y, u1.x, u1.y);
+                    Four<T>::store(dst + at1, v0.x, v0.y, v1.x, v1.y);
+                }
             }
         }
     }
