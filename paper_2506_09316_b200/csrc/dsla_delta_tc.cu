@@ -560,45 +560,37 @@ template <int THREADS> __device__ __forceinline__ void item_wait(int id) { asm v
 template <int THREADS> __device__ __forceinline__ void item_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
 constexpr int PUBLISHED = 3, READ = 5;
 
-template <int D, int W>
-__global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
-                                                                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
-    using L = Walk<D, W>;
-    using In = Chunk<D>;
-    constexpr bool MORE = W > 32;      // slabs of 32 columns are for grids that fit on the device at once
-    constexpr int SLABS = D / W, MMA_WARP = L::ROW_WARPS, LOAD_WARP = MMA_WARP + 1;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free;
-    __shared__ __align__(16) uint8_t answer[16];
-    __shared__ uint64_t answered;
-    __shared__ Item items[2];
-    __shared__ uint8_t order[128];
-    __shared__ uint32_t tmem_base;
-    __shared__ int abort_flag;
-    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
-    const DeltaParams& p = tp.p;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    volatile int* abortp = &abort_flag;
+struct WalkShared {
+    __align__(16) uint8_t answer[16];
+    uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free, answered;
+    Item items[2];
+    uint8_t order[128];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+// Barriers, tensor memory, and the order of the sequences; returns whether there is one.  `y_readers`: warps that arrive when they have read a stage of Y.
+template <class L>
+__device__ __forceinline__ bool walk_set_up(WalkShared& sh, const DeltaParams& p, int tid, int warp, int y_readers) {
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
-            mbar_init(&kq_full[i], 1);
-            mbar_init(&kq_empty[i], 1);
-            mbar_init(&y_full[i], 1);
-            mbar_init(&y_empty[i], 1 + L::ROW_WARPS / 2);      // the MMAs, and the warps that read the gates off the chain
+            mbar_init(&sh.kq_full[i], 1);
+            mbar_init(&sh.kq_empty[i], 1);
+            mbar_init(&sh.y_full[i], 1);
+            mbar_init(&sh.y_empty[i], 1 + y_readers);
         }
-        mbar_init(&answered, 1);
-        mbar_init(&x_full, 1);
-        mbar_init(&d_full, 1);
-        mbar_init(&o_full, 1);
-        mbar_init(&o_free, L::ROW_WARPS / 2);
-        abort_flag = 0;
+        mbar_init(&sh.answered, 1);
+        mbar_init(&sh.x_full, 1);
+        mbar_init(&sh.d_full, 1);
+        mbar_init(&sh.o_full, 1);
+        mbar_init(&sh.o_free, L::ROW_WARPS / 2);
+        sh.abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == MMA_WARP) { tmem_alloc(&tmem_base, L::COLS); tmem_relinquish(); }
+    if (warp == L::ROW_WARPS) { tmem_alloc(&sh.tmem_base, L::COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tb = tmem_base;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const bool sorted = p.cu_seqlens && p.N > 1 && p.N <= 128;
@@ -611,65 +603,92 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
                 rank += other > mine || (other == mine && k < tid);
                 from = to;
             }
-            order[rank] = (uint8_t)tid;
+            sh.order[rank] = (uint8_t)tid;
         }
         __syncthreads();
     }
+    return sorted;
+}
+
+// The loading warp.
+template <class L>
+__device__ __forceinline__ void walk_load(WalkShared& sh, const CUtensorMap& map_k, const CUtensorMap& map_q, const CUtensorMap& map_v, const DeltaTcParams& tp, uint8_t* sm, bool sorted,
+                                          int lane) {
+    using In = typename L::In;
+    constexpr bool MORE = L::W > 32;      // slabs of 32 columns are for grids that fit on the device at once
+    constexpr int D = L::D, W = L::W, SLABS = D / W;
+    const DeltaParams& p = tp.p;
+    volatile int* abortp = &sh.abort_flag;
+    int block = blockIdx.x, cc = 0;      // cc: chunks of all items so far
+    for (int it = 0;; ++it) {
+        Item x{};
+        x.chunks = -1;
+        if (block >= 0) {
+            if (MORE && lane == 0) ask_for_next(sh.answer, &sh.answered);
+            const int place = block / (SLABS * p.H), n = sorted ? sh.order[place] : place;
+            find_sequence(tp, n, x.t_begin, x.len, x.first);
+            x.slot = p.slots ? p.slots[n] : n;
+            x.h = (block / SLABS) % p.H;
+            x.column = block % SLABS * W;
+            x.live = x.slot >= 0 && x.slot < p.num_slots && (x.len > 0 || !p.use_initial_state);
+            x.chunks = x.live ? (x.len + DC - 1) / DC : 0;
+        }
+        if (it >= 2) item_wait<L::THREADS>(READ + (it & 1));
+        if (lane == 0) sh.items[it & 1] = x;
+        __syncwarp();
+        item_arrive<L::THREADS>(PUBLISHED + (it & 1));
+        if (block < 0) break;
+        if (x.live && p.use_initial_state)      // rows of the state, on their way before they are asked for
+            for (int i = lane; i < D; i += 32)
+                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.state + (((size_t)x.slot * p.H + x.h) * D + i) * D + x.column), "n"(W * 4) : "memory");
+        if (lane == 0) {
+            const int hq = x.h / p.group;
+            for (int c = 0; c < x.chunks && !*abortp; ++c, ++cc) {
+                const int st = cc % ST, t = x.t_begin + c * DC;
+                if (cc >= ST) WAIT(&sh.kq_empty[st], (cc / ST - 1) & 1);
+                uint8_t* to = sm + st * L::KQ;
+                mbar_arrive_expect_tx(&sh.kq_full[st], L::KQ);
+                for (int half = 0; half < D / 64; ++half) {
+                    tma_load_4d(to + half * 2 * TILE, &map_k, &sh.kq_full[st], 0, t, half, hq);
+                    tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &sh.kq_full[st], 0, t, half, hq);
+                }
+                if (cc >= ST) WAIT(&sh.y_empty[st], (cc / ST - 1) & 1);
+                to = sm + L::OFF_Y + st * L::Y_STAGE;
+                mbar_arrive_expect_tx(&sh.y_full[st], L::Y_BYTES);
+                bulk_load(to, tp.ws + ((size_t)(x.first + c) * p.H + x.h) * In::BYTES, In::BYTES, &sh.y_full[st]);
+                for (int col = 0; col < W; col += 64) tma_load_3d(to + L::V + col / 64 * TILE, &map_v, &sh.y_full[st], x.column + col, x.h, t);
+            }
+        }
+        __syncwarp();
+        block = -1;
+        if (MORE) {
+            WAIT(&sh.answered, it & 1);
+            block = __shfl_sync(0xffffffffu, *abortp ? -1 : next_block(sh.answer), 0);
+        }
+    }
+}
+
+template <int D, int W>
+__global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
+                                                                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
+    using L = Walk<D, W>;
+    using In = Chunk<D>;
+    constexpr int MMA_WARP = L::ROW_WARPS, LOAD_WARP = MMA_WARP + 1;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ WalkShared sh;
+    uint64_t *kq_full = sh.kq_full, *kq_empty = sh.kq_empty, *y_full = sh.y_full, *y_empty = sh.y_empty;
+    uint64_t &x_full = sh.x_full, &d_full = sh.d_full, &o_full = sh.o_full, &o_free = sh.o_free;
+    Item* items = sh.items;
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
+    const DeltaParams& p = tp.p;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abortp = &sh.abort_flag;
+    const bool sorted = walk_set_up<L>(sh, p, tid, warp, L::ROW_WARPS / 2);      // half of the rows read the gates of a stage off the chain
+    const uint32_t tb = sh.tmem_base;
 
     if (warp == LOAD_WARP) {
-        if (lane == 0) {
-            prefetch_tensormap(&map_k);
-            prefetch_tensormap(&map_q);
-            prefetch_tensormap(&map_v);
-            prefetch_tensormap(&map_o);
-        }
-        int block = blockIdx.x, cc = 0;      // cc: chunks of all items so far
-        for (int it = 0;; ++it) {
-            Item x{};
-            x.chunks = -1;
-            if (block >= 0) {
-                if (MORE && lane == 0) ask_for_next(answer, &answered);
-                const int place = block / (SLABS * p.H), n = sorted ? order[place] : place;
-                find_sequence(tp, n, x.t_begin, x.len, x.first);
-                x.slot = p.slots ? p.slots[n] : n;
-                x.h = (block / SLABS) % p.H;
-                x.column = block % SLABS * W;
-                x.live = x.slot >= 0 && x.slot < p.num_slots && (x.len > 0 || !p.use_initial_state);
-                x.chunks = x.live ? (x.len + DC - 1) / DC : 0;
-            }
-            if (it >= 2) item_wait<L::THREADS>(READ + (it & 1));
-            if (lane == 0) items[it & 1] = x;
-            __syncwarp();
-            item_arrive<L::THREADS>(PUBLISHED + (it & 1));
-            if (block < 0) break;
-            if (x.live && p.use_initial_state)      // rows of the state, on their way before they are asked for
-                for (int i = lane; i < D; i += 32)
-                    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.state + (((size_t)x.slot * p.H + x.h) * D + i) * D + x.column), "n"(W * 4) : "memory");
-            if (lane == 0) {
-                const int hq = x.h / p.group;
-                for (int c = 0; c < x.chunks && !*abortp; ++c, ++cc) {
-                    const int st = cc % ST;
-                    if (cc >= ST) WAIT(&kq_empty[st], (cc / ST - 1) & 1);
-                    uint8_t* to = sm + st * L::KQ;
-                    mbar_arrive_expect_tx(&kq_full[st], L::KQ);
-                    for (int half = 0; half < D / 64; ++half) {
-                        tma_load_4d(to + half * 2 * TILE, &map_k, &kq_full[st], 0, x.t_begin + c * DC, half, hq);
-                        tma_load_4d(to + half * 2 * TILE + TILE, &map_q, &kq_full[st], 0, x.t_begin + c * DC, half, hq);
-                    }
-                    if (cc >= ST) WAIT(&y_empty[st], (cc / ST - 1) & 1);
-                    to = sm + L::OFF_Y + st * L::Y_STAGE;
-                    mbar_arrive_expect_tx(&y_full[st], L::Y_BYTES);
-                    bulk_load(to, tp.ws + ((size_t)(x.first + c) * p.H + x.h) * In::BYTES, In::BYTES, &y_full[st]);
-                    tma_load_3d(to + L::V, &map_v, &y_full[st], x.column, x.h, x.t_begin + c * DC);
-                }
-            }
-            __syncwarp();
-            block = -1;
-            if (MORE) {
-                WAIT(&answered, it & 1);
-                block = __shfl_sync(0xffffffffu, *abortp ? -1 : next_block(answer), 0);
-            }
-        }
+        if (lane == 0) prefetch_tensormap(&map_o);
+        walk_load<L>(sh, map_k, map_q, map_v, tp, sm, sorted, lane);
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
         constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1);
@@ -853,6 +872,273 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     if (warp == MMA_WARP) tmem_dealloc(tb, L::COLS);
 }
 
+// The walk with a whole head of d = 128 to a CTA, everything turned over: lanes of TMEM are columns of d_v.  S^T and R^T are A operands in tensor memory, two terms each, so only
+// K, Q, Y and P T, the B operands, pass through shared memory, once for all 128 columns:
+//   S^T [K; Q]^T            128 x 128 x 128, two terms    columns 0..63 (K S)^T, 64..127 (Q S)^T
+//   R^T Y^T                 128 x 128 x 64, three products of terms (low by low left out: 2^-18); on the chain
+//   scale G (Q S)^T + R^T (P T)^T    128 x 64 x 64, two terms, onto what the rows put there; behind it
+// Sixteen row warps, four to a lane quadrant ("parts"): each has 32 columns of d_k of the state in registers; parts 0 and 1 make R of 32 tokens each, 2 and 3 scale Q S and finish
+// the outputs of the chunk before.  V comes transposed through ldmatrix in the fragment layout that R is then stored in, outputs leave through stmatrix.
+struct Wide {
+    using In = Chunk<128>;
+    static constexpr int D = 128, W = 128, ROW_WARPS = 16, THREADS = 32 * (ROW_WARPS + 2);
+    static constexpr int KQ = 4 * TILE, V = (In::BYTES + 1023) & ~1023, Y_STAGE = V + 2 * TILE, OFF_Y = ST * KQ, OFF_O = OFF_Y + ST * Y_STAGE, SMEM = OFF_O + 8 * 2048 + 1024;
+    static constexpr uint32_t COL_SH = 0, COL_SL = 64, COL_RH = 128, COL_RL = 160, COL_O = 192, COL_X = 256, COL_D = 384, COLS = 512;
+    static constexpr uint32_t Y_BYTES = In::BYTES + 2 * TILE;
+};
+
+// A pair of fp32 in two bf16 terms.
+__device__ __forceinline__ void split_pair(uint64_t x, uint32_t& hi, uint32_t& lo) {
+    const float2 y = unpair(x);
+    hi = pack_bf16(y.x, y.y);
+    const float2 z = unpair(add2(x, pair((hi << 16) ^ 0x80000000u, (hi & 0xffff0000u) ^ 0x80000000u)));
+    lo = pack_bf16(z.x, z.y);
+}
+
+__global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
+                                                                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
+    using L = Wide;
+    using In = L::In;
+    constexpr int D = L::D, MMA_WARP = L::ROW_WARPS, LOAD_WARP = MMA_WARP + 1;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ WalkShared sh;
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
+    const DeltaParams& p = tp.p;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abortp = &sh.abort_flag;
+    const bool sorted = walk_set_up<L>(sh, p, tid, warp, 0);
+    const uint32_t tb = sh.tmem_base;
+
+    if (warp == LOAD_WARP) {
+        if (lane == 0) prefetch_tensormap(&map_o);
+        walk_load<L>(sh, map_k, map_q, map_v, tp, sm, sorted, lane);
+    } else if (warp == MMA_WARP) {
+        const uint32_t base = smem_u32(sm);
+        constexpr uint32_t ID = idesc_bf16(128, 128, 0, 0), ID_O = idesc_bf16(128, 64, 0, 0);
+        int c = 0;      // chunks of all items
+        for (int it = 0;; ++it) {
+            item_wait<L::THREADS>(PUBLISHED + (it & 1));
+            const int chunks = sh.items[it & 1].chunks;
+            __syncwarp();
+            if (chunks < 0) break;
+            item_arrive<L::THREADS>(READ + (it & 1));
+            for (const int end = c + chunks; c < end; ++c) {
+                const int st = c % ST;
+                const uint32_t kq = base + st * L::KQ, y = base + L::OFF_Y + st * L::Y_STAGE;
+                WAIT(&sh.kq_full[st], (c / ST) & 1);
+                rows_wait<1, L::ROW_WARPS>();
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 1; k >= 0; --k)
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk)
+                            mma_ts(tb + L::COL_X, tb + (k ? L::COL_SL : L::COL_SH) + 8 * kk, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), ID, !k || kk ? 1u : 0u);
+                    tc_commit(&sh.x_full);
+                    tc_commit(&sh.kq_empty[st]);
+                }
+                __syncwarp();
+                WAIT(&sh.y_full[st], (c / ST) & 1);
+                rows_wait<2, L::ROW_WARPS / 2>();
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 2; k >= 0; --k)      // R_hi Y_lo, R_lo Y_hi, R_hi Y_hi
+#pragma unroll
+                        for (int kk = 0; kk < DC / 16; ++kk)
+                            mma_ts(tb + L::COL_D, tb + (k == 1 ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + (k == 2 ? In::Y : 0) + kk * 32, 16, 1024), ID, k < 2 || kk ? 1u : 0u);
+                    tc_commit(&sh.d_full);
+                }
+                __syncwarp();
+                rows_wait<7, L::ROW_WARPS / 2>();
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 1; k >= 0; --k)
+#pragma unroll
+                        for (int kk = 0; kk < DC / 16; ++kk)
+                            mma_ts(tb + L::COL_O, tb + (k ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + In::PT + kk * 32, 16, 1024), ID_O, 1u);
+                    tc_commit(&sh.o_full);
+                    tc_commit(&sh.y_empty[st]);
+                }
+                __syncwarp();
+            }
+        }
+    } else {
+        const int quad = warp & 3, part = warp >> 2, m = lane >> 3;
+        const uint32_t lane_addr = tb + ((uint32_t)(32 * quad) << 16);
+        const bool makes_r = part < 2;
+        const int tok = 32 * (part & 1);      // this warp's tokens of a chunk: R's, or the outputs'
+        uint64_t s[16];                       // S^T: columns 32 part .. of d_k
+        int cc = 0;                           // chunks of all items so far
+        uint8_t* o_tile = sm + L::OFF_O + (quad + 4 * (part & 1)) * 2048;      // 32 tokens x 32 columns, rows of 64 bytes, swizzled
+        // The outputs of chunk c (parts 2, 3), the latest of all.  Whole rows of 32 tokens leave by a TMA store of this warp, those of a ragged end row by row.
+        auto outputs = [&](const Item& x, int c) {
+            uint32_t v[2][16];
+            WAIT_HOT(&sh.o_full, (cc - 1) & 1);
+            tc_fence_after();
+            tmem_ld_16x256b_x4(lane_addr + L::COL_O + tok, v[0]);
+            tmem_ld_16x256b_x4(lane_addr + (16u << 16) + L::COL_O + tok, v[1]);
+            tc_wait_ld();
+            tc_fence_before();
+            const int t0 = c * DC + tok;
+            if (t0 >= x.len) return;
+            if (lane == 0) bulk_wait_read();
+            __syncwarp();
+            uint32_t z[2][8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[half][i] = pack_bf16(__uint_as_float(v[half][2 * i]), __uint_as_float(v[half][2 * i + 1]));
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const int r = 8 * (i + (m >> 1)) + (lane & 7);
+                    stmatrix_x4_trans(smem_u32(o_tile) + r * 64 + (((2 * half + (m & 1)) ^ ((r >> 1) & 3)) << 4), z[half][2 * i], z[half][2 * i + 1], z[half][2 * i + 2], z[half][2 * i + 3]);
+                }
+            if (t0 + 32 <= x.len) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_3d(&map_o, o_tile, 32 * quad, x.h, x.t_begin + t0);
+                    bulk_commit();
+                }
+            } else {
+                __syncwarp();
+                if (t0 + lane < x.len) {
+                    uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(x.t_begin + t0 + lane) * p.H + x.h) * D + 32 * quad);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[i] = *reinterpret_cast<const uint4*>(o_tile + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4));
+                }
+            }
+        };
+        for (int it = 0;; ++it) {
+            item_wait<L::THREADS>(PUBLISHED + (it & 1));
+            const Item x = sh.items[it & 1];
+            __syncwarp();
+            if (x.chunks < 0) break;
+            item_arrive<L::THREADS>(READ + (it & 1));
+            float* S = p.state + (((size_t)x.slot * p.H + x.h) * D + 32 * part) * D + 32 * quad + lane;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = x.live && p.use_initial_state ? pair(S[2 * i * D], S[(2 * i + 1) * D]) : 0;
+            for (int c = 0; c < x.chunks; ++c, ++cc) {
+                const int st = cc % ST, live = min(DC, x.len - c * DC);
+                const uint8_t* stage = sm + L::OFF_Y + st * L::Y_STAGE;
+                const float* meta = reinterpret_cast<const float*>(stage + In::META);
+                {
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) split_pair(s[i], hi[i], lo[i]);
+                    tmem_st16(lane_addr + L::COL_SH + 16 * part, hi);
+                    tmem_st16(lane_addr + L::COL_SL + 16 * part, lo);
+                    tc_wait_st();
+                }
+                tc_fence_before();
+                rows_arrive<1, L::ROW_WARPS>();
+                float last;
+                if (makes_r) {
+                    WAIT_HOT(&sh.y_full[st], (cc / ST) & 1);
+                    last = meta[2 * DC - 1];
+                    uint64_t G[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 g = *reinterpret_cast<const float2*>(meta + DC + tok + 8 * i + 2 * (lane & 3));
+                        G[i] = pair(-g.x, -g.y);
+                    }
+                    uint32_t vr[2][8];      // V^T in the fragment layout
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const int r = tok + 8 * (i + (m >> 1)) + (lane & 7), piece = 4 * (quad & 1) + 2 * half + (m & 1);
+                            ldmatrix_x4_trans(smem_u32(stage) + L::V + (quad >> 1) * TILE + r * 128 + ((piece ^ (r & 7)) << 4), vr[half][2 * i], vr[half][2 * i + 1], vr[half][2 * i + 2],
+                                              vr[half][2 * i + 3]);
+                        }
+                    WAIT_HOT(&sh.x_full, cc & 1);
+                    tc_fence_after();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t at = lane_addr + ((uint32_t)(16 * half) << 16);
+                        uint32_t a[16];
+                        tmem_ld_16x256b_x4(at + L::COL_X + tok, a);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t hi[2], lo[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t word = vr[half][2 * i + e];
+                                uint64_t r = fma2(G[i], pair(a[4 * i + 2 * e], a[4 * i + 2 * e + 1]), pair(word << 16, word & 0xffff0000u));
+                                if (live < DC) {      // tokens behind the sequence's end, whatever they hold
+                                    const int j = tok + 8 * i + 2 * (lane & 3);
+                                    const float2 u = unpair(r);
+                                    r = pair(j < live ? u.x : 0.f, j + 1 < live ? u.y : 0.f);
+                                }
+                                split_pair(r, hi[e], lo[e]);
+                            }
+                            tmem_st_16x128b(at + L::COL_RH + tok / 2 + 4 * i, hi[0], hi[1]);
+                            tmem_st_16x128b(at + L::COL_RL + tok / 2 + 4 * i, lo[0], lo[1]);
+                        }
+                    }
+                    tc_wait_st();
+                    tc_fence_before();
+                    rows_arrive<2, L::ROW_WARPS / 2>();
+                } else {
+                    if (c > 0) outputs(x, c - 1);
+                    WAIT_HOT(&sh.y_full[st], (cc / ST) & 1);
+                    last = meta[2 * DC - 1];
+                    WAIT_HOT(&sh.x_full, cc & 1);
+                    tc_fence_after();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t a[16];
+                        tmem_ld16(lane_addr + L::COL_X + DC + tok + 16 * half, a);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const float4 g = *reinterpret_cast<const float4*>(meta + tok + 16 * half + i);
+                            a[i] = __float_as_uint(__uint_as_float(a[i]) * g.x);
+                            a[i + 1] = __float_as_uint(__uint_as_float(a[i + 1]) * g.y);
+                            a[i + 2] = __float_as_uint(__uint_as_float(a[i + 2]) * g.z);
+                            a[i + 3] = __float_as_uint(__uint_as_float(a[i + 3]) * g.w);
+                        }
+                        tmem_st16(lane_addr + L::COL_O + tok + 16 * half, a);
+                    }
+                    tc_wait_st();
+                    tc_fence_before();
+                    rows_arrive<7, L::ROW_WARPS / 2>();
+                }
+                WAIT_HOT(&sh.d_full, cc & 1);
+                tc_fence_after();
+                const uint64_t keep = pair(last, last);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t a[16];
+                    tmem_ld16(lane_addr + L::COL_D + 32 * part + 16 * half, a);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[8 * half + i] = fma2(keep, s[8 * half + i], pair(a[2 * i], a[2 * i + 1]));
+                }
+            }
+            if (!makes_r && x.chunks > 0) outputs(x, x.chunks - 1);
+            if (x.live) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 u = unpair(s[i]);
+                    S[2 * i * D] = u.x;
+                    S[(2 * i + 1) * D] = u.y;
+                }
+            }
+        }
+        if (lane == 0) bulk_wait_read();
+    }
+    tc_fence_before();
+    __syncthreads();
+    settle_after_timeout(abortp);
+    if (warp == MMA_WARP) tmem_dealloc(tb, L::COLS);
+}
+
 // [T_total, H_qk, D] bf16 as (64 elements, t, part of a row, head); a box is 64 tokens of one part, one swizzled tile.
 bool make_map(CUtensorMap* m, const void* base, int T_total, int H, int d) {
     cuuint64_t dims[4] = {64, (cuuint64_t)T_total, (cuuint64_t)(d / 64), (cuuint64_t)H};
@@ -873,19 +1159,21 @@ long long chunk_slots(const dsla_delta_prefill_args* a) {
     return a->cu_seqlens ? (long long)a->T_total / DC + a->N : (long long)a->N * ((a->T + DC - 1) / DC);
 }
 
-template <int D, int W>
-dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CUtensorMap& mq, const CUtensorMap& mo, const DeltaTcParams& tp, int T_total) {
-    using L = Walk<D, W>;
+template <class L, class Kernel>
+dsla_status launch_walk(cudaLaunchConfig_t& cfg, Kernel kernel, const CUtensorMap& mk, const CUtensorMap& mq, const DeltaTcParams& tp, int T_total) {
     const DeltaParams& p = tp.p;
-    CUtensorMap mv{};
-    if (T_total > 0 && !make_slab_map(&mv, p.v, T_total, p.H, D, W, DC, W == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B)) return DSLA_ERR_CUDA;
-    const long long ctas = (long long)p.N * p.H * (D / W);
+    const int v_columns = L::W < 64 ? L::W : 64, o_columns = L::W == 128 ? 32 : WC;
+    CUtensorMap mv{}, mo{};
+    if (T_total > 0 && (!make_slab_map(&mv, p.v, T_total, p.H, L::D, v_columns, DC, v_columns == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B) ||
+                        !make_slab_map(&mo, p.o, T_total, p.H, L::D, o_columns, 32, o_columns == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE)))
+        return DSLA_ERR_CUDA;
+    const long long ctas = (long long)p.N * p.H * (L::D / L::W);
     if (ctas > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(delta_walk_kernel<D, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(L::THREADS);
     cfg.dynamicSmemBytes = L::SMEM;
-    if (cudaLaunchKernelEx(&cfg, delta_walk_kernel<D, W>, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kernel, mk, mq, mv, mo, tp) != cudaSuccess) return DSLA_ERR_CUDA;
     count_launch();
     return DSLA_OK;
 }
@@ -893,10 +1181,8 @@ dsla_status launch_walk(cudaLaunchConfig_t& cfg, const CUtensorMap& mk, const CU
 template <int D>
 dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cudaStream_t s) {
     const DeltaParams& p = tp.p;
-    CUtensorMap mk{}, mq{}, mo{};
-    if (a->T_total > 0 && (!make_map(&mk, p.k, a->T_total, a->H_qk, D) || !make_map(&mq, p.q, a->T_total, a->H_qk, D) ||
-                           !make_slab_map(&mo, p.o, a->T_total, p.H, D, WC, 32, CU_TENSOR_MAP_SWIZZLE_NONE)))
-        return DSLA_ERR_CUDA;
+    CUtensorMap mk{}, mq{};
+    if (a->T_total > 0 && (!make_map(&mk, p.k, a->T_total, a->H_qk, D) || !make_map(&mq, p.q, a->T_total, a->H_qk, D))) return DSLA_ERR_CUDA;
     const long long prep = a->T_total > 0 ? (long long)tp.slots * p.H : 0;
     if (prep > 0x7fffffffLL) return DSLA_ERR_UNSUPPORTED;
     if (cudaFuncSetAttribute(delta_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Prep<D>::SMEM) != cudaSuccess) return DSLA_ERR_CUDA;
@@ -916,8 +1202,10 @@ dsla_status launch(const DeltaTcParams& tp, const dsla_delta_prefill_args* a, cu
     } else {
         cfg.numAttrs = 0;      // not ahead of whatever kernel comes before: it may still want tensor memory
     }
-    const dsla_status rc = (long long)p.N * p.H * (D / 32) <= sm_count() ? launch_walk<D, 32>(cfg, mk, mq, mo, tp, a->T_total)
-                                                                           : launch_walk<D, 64>(cfg, mk, mq, mo, tp, a->T_total);
+    dsla_status rc;
+    if ((long long)p.N * p.H * (D / 32) <= sm_count()) rc = launch_walk<Walk<D, 32>>(cfg, delta_walk_kernel<D, 32>, mk, mq, tp, a->T_total);
+    else if constexpr (D == 128) rc = launch_walk<Wide>(cfg, delta_walk_wide_kernel, mk, mq, tp, a->T_total);
+    else rc = launch_walk<Walk<D, 64>>(cfg, delta_walk_kernel<D, 64>, mk, mq, tp, a->T_total);
     if (rc != DSLA_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? DSLA_OK : DSLA_ERR_CUDA;
 }
