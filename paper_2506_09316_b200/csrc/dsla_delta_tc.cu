@@ -563,6 +563,7 @@ constexpr int PUBLISHED = 3, READ = 5;
 struct WalkShared {
     __align__(16) uint8_t answer[16];
     uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free, answered;
+    uint64_t q_full, d2_full;      // a whole head to a CTA: Q S, and the second half of the state's columns
     Item items[2];
     uint8_t order[128];
     uint32_t tmem_base;
@@ -581,6 +582,8 @@ __device__ __forceinline__ bool walk_set_up(WalkShared& sh, const DeltaParams& p
         }
         mbar_init(&sh.answered, 1);
         mbar_init(&sh.x_full, 1);
+        mbar_init(&sh.q_full, 1);
+        mbar_init(&sh.d2_full, 1);
         mbar_init(&sh.d_full, 1);
         mbar_init(&sh.o_full, 1);
         mbar_init(&sh.o_free, L::ROW_WARPS / 2);
@@ -914,7 +917,15 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
         walk_load<L>(sh, map_k, map_q, map_v, tp, sm, sorted, lane);
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm);
-        constexpr uint32_t ID = idesc_bf16(128, 128, 0, 0), ID_O = idesc_bf16(128, 64, 0, 0);
+        constexpr uint32_t ID = idesc_bf16(128, 64, 0, 0);
+        // S^T times 64 rows of K or Q, 64 channels of d_k from 16 `from` on, both terms of S.
+        auto products = [&](uint32_t rows, int from, uint32_t add, uint32_t to = L::COL_X) {
+#pragma unroll
+            for (int k = 1; k >= 0; --k)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_ts(tb + to, tb + (k ? L::COL_SL : L::COL_SH) + 8 * (from + kk), smem_desc_sw128(rows + (from / 4) * 2 * TILE + kk * 32, 16, 1024), ID, !k || kk ? 1u : add);
+        };
         int c = 0;      // chunks of all items
         for (int it = 0;; ++it) {
             item_wait<L::THREADS>(PUBLISHED + (it & 1));
@@ -926,15 +937,20 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                 const int st = c % ST;
                 const uint32_t kq = base + st * L::KQ, y = base + L::OFF_Y + st * L::Y_STAGE;
                 WAIT(&sh.kq_full[st], (c / ST) & 1);
-                rows_wait<1, L::ROW_WARPS>();
+                rows_wait<1, L::ROW_WARPS / 2>();
                 tc_fence_after();
                 if (elect_one()) {
-#pragma unroll
-                    for (int k = 1; k >= 0; --k)
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk)
-                            mma_ts(tb + L::COL_X, tb + (k ? L::COL_SL : L::COL_SH) + 8 * kk, smem_desc_sw128(kq + (kk / 4) * 2 * TILE + (kk % 4) * 32, 16, 1024), ID, !k || kk ? 1u : 0u);
+                    products(kq, 0, 0);
+                }
+                __syncwarp();
+                rows_wait<8, L::ROW_WARPS / 2>();
+                tc_fence_after();
+                if (elect_one()) {
+                    products(kq, 4, 1);
                     tc_commit(&sh.x_full);
+                    products(kq + TILE, 0, 0, L::COL_X + DC);
+                    products(kq + TILE, 4, 1, L::COL_X + DC);
+                    tc_commit(&sh.q_full);
                     tc_commit(&sh.kq_empty[st]);
                 }
                 __syncwarp();
@@ -943,11 +959,15 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 2; k >= 0; --k)      // R_hi Y_lo, R_lo Y_hi, R_hi Y_hi
+                    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                        for (int kk = 0; kk < DC / 16; ++kk)
-                            mma_ts(tb + L::COL_D, tb + (k == 1 ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + (k == 2 ? In::Y : 0) + kk * 32, 16, 1024), ID, k < 2 || kk ? 1u : 0u);
-                    tc_commit(&sh.d_full);
+                        for (int k = 2; k >= 0; --k)      // R_hi Y_lo, R_lo Y_hi, R_hi Y_hi
+#pragma unroll
+                            for (int kk = 0; kk < DC / 16; ++kk)
+                                mma_ts(tb + L::COL_D + 64 * half, tb + (k == 1 ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + (k == 2 ? In::Y : 0) + half * TILE + kk * 32, 16, 1024),
+                                       ID, k < 2 || kk ? 1u : 0u);
+                        tc_commit(half ? &sh.d2_full : &sh.d_full);
+                    }
                 }
                 __syncwarp();
                 rows_wait<7, L::ROW_WARPS / 2>();
@@ -957,7 +977,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                     for (int k = 1; k >= 0; --k)
 #pragma unroll
                         for (int kk = 0; kk < DC / 16; ++kk)
-                            mma_ts(tb + L::COL_O, tb + (k ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + In::PT + kk * 32, 16, 1024), ID_O, 1u);
+                            mma_ts(tb + L::COL_O, tb + (k ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + In::PT + kk * 32, 16, 1024), ID, 1u);
                     tc_commit(&sh.o_full);
                     tc_commit(&sh.y_empty[st]);
                 }
@@ -1035,7 +1055,8 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                     tc_wait_st();
                 }
                 tc_fence_before();
-                rows_arrive<1, L::ROW_WARPS>();
+                if (makes_r) rows_arrive<1, L::ROW_WARPS / 2>();
+                else rows_arrive<8, L::ROW_WARPS / 2>();
                 float last;
                 if (makes_r) {
                     WAIT_HOT(&sh.y_full[st], (cc / ST) & 1);
@@ -1088,7 +1109,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                     if (c > 0) outputs(x, c - 1);
                     WAIT_HOT(&sh.y_full[st], (cc / ST) & 1);
                     last = meta[2 * DC - 1];
-                    WAIT_HOT(&sh.x_full, cc & 1);
+                    WAIT_HOT(&sh.q_full, cc & 1);
                     tc_fence_after();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -1109,7 +1130,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                     tc_fence_before();
                     rows_arrive<7, L::ROW_WARPS / 2>();
                 }
-                WAIT_HOT(&sh.d_full, cc & 1);
+                WAIT_HOT(makes_r ? &sh.d_full : &sh.d2_full, cc & 1);
                 tc_fence_after();
                 const uint64_t keep = pair(last, last);
 #pragma unroll
