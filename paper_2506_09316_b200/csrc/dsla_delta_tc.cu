@@ -67,11 +67,15 @@ __device__ __forceinline__ void find_sequence(const DeltaTcParams& tp, int n, in
     }
 }
 
-// x in two bf16 terms, high and low.
-__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
-    hi = pack_bf16(x, y);
-    const float2 h = unpack_bf16(hi);
-    lo = pack_bf16(x - h.x, y - h.y);
+// A pair of fp32 in bf16, and what that leaves; and in two bf16 terms, high and low.
+__device__ __forceinline__ uint64_t take_bf16(uint64_t x, uint32_t& hi) {
+    const float2 y = unpair(x);
+    hi = pack_bf16(y.x, y.y);
+    return add2(x, pair((hi << 16) ^ 0x80000000u, (hi & 0xffff0000u) ^ 0x80000000u));
+}
+__device__ __forceinline__ void split_pair(uint64_t x, uint32_t& hi, uint32_t& lo) {
+    const float2 z = unpair(take_bf16(x, hi));
+    lo = pack_bf16(z.x, z.y);
 }
 
 #define WAIT(bar, parity) mbar_wait(bar, parity, abortp, p.status)
@@ -105,7 +109,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
     __shared__ uint64_t full, done;
     __shared__ uint32_t tmem_base;
     __shared__ int abort_flag;
-    __shared__ __align__(16) float lhi[DC], llo[DC], sbeta[DC], sw[DC], sleft[DC / 2];
+    __shared__ __align__(16) float mhi[DC], mlo[DC], sbeta[DC], sw[DC], sleft[DC / 2];
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
     uint8_t* work = sm + L::KQ;
     const DeltaParams& p = tp.p;
@@ -183,8 +187,8 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * lane + i;
             const float hi = (float)run[i], G = ex2(hi);
-            lhi[j] = hi;
-            llo[j] = (float)(run[i] - hi);
+            mhi[j] = -hi;      // minus the sums: differences are additions
+            mlo[j] = (float)(hi - run[i]);
             sbeta[j] = beta[i];
             sw[j] = ex2((float)(last - run[i]));
             if (j < 32) sleft[j] = ex2((float)(middle - run[i]));
@@ -222,40 +226,45 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) *reinterpret_cast<uint4*>(sm + half * 2 * TILE + i * 16) = make_uint4(0u, 0u, 0u, 0u);
     if (upper >= part) {
-        const float f = j < live ? (is_p ? p.scale : sbeta[j]) : 0.f, hj = lhi[j], lj = llo[j];
-        const float fr = f * ex2((hj - lhi[31]) + (lj - llo[31]));      // left of a diagonal block of 32: through the sum up to token 31
+        const float f = j < live ? (is_p ? p.scale : sbeta[j]) : 0.f, hj = -mhi[j], lj = -mlo[j];
+        const float fr = f * ex2((hj + mhi[31]) + (lj + mlo[31]));      // left of a diagonal block of 32: through the sum up to token 31
         const int last = j >= live ? -1 : is_p ? j : j - 1;             // columns up to this one
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int c0 = 32 * part + 16 * half;
             uint32_t r[16];
-            float x[16];
+            uint64_t x[8];
             tmem_ld16(row_addr + 16 * half, r);
             tc_wait_ld();
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                float4 e;
+                uint64_t e[2];
                 if (upper == part) {
-                    const float4 hs = *reinterpret_cast<const float4*>(lhi + c0 + i), ls = *reinterpret_cast<const float4*>(llo + c0 + i);
-                    e = make_float4(f * ex2((hj - hs.x) + (lj - ls.x)), f * ex2((hj - hs.y) + (lj - ls.y)), f * ex2((hj - hs.z) + (lj - ls.z)), f * ex2((hj - hs.w) + (lj - ls.w)));
+                    const ulonglong2 hs = *reinterpret_cast<const ulonglong2*>(mhi + c0 + i), ls = *reinterpret_cast<const ulonglong2*>(mlo + c0 + i);
+                    const float2 u = unpair(add2(add2(pair(hj, hj), hs.x), add2(pair(lj, lj), ls.x))), v = unpair(add2(add2(pair(hj, hj), hs.y), add2(pair(lj, lj), ls.y)));
+                    e[0] = mul2(pair(f, f), pair(ex2(u.x), ex2(u.y)));
+                    e[1] = mul2(pair(f, f), pair(ex2(v.x), ex2(v.y)));
                 } else {
-                    const float4 l = *reinterpret_cast<const float4*>(sleft + c0 + i);
-                    e = make_float4(fr * l.x, fr * l.y, fr * l.z, fr * l.w);
+                    const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(sleft + c0 + i);
+                    e[0] = mul2(pair(fr, fr), l.x);
+                    e[1] = mul2(pair(fr, fr), l.y);
                 }
-                x[i] = c0 + i <= last ? __uint_as_float(r[i]) * e.x : 0.f;
-                x[i + 1] = c0 + i + 1 <= last ? __uint_as_float(r[i + 1]) * e.y : 0.f;
-                x[i + 2] = c0 + i + 2 <= last ? __uint_as_float(r[i + 2]) * e.z : 0.f;
-                x[i + 3] = c0 + i + 3 <= last ? __uint_as_float(r[i + 3]) * e.w : 0.f;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = i + 2 * k;
+                    const float2 y = unpair(mul2(pair(r[at], r[at + 1]), e[k]));
+                    x[at / 2] = pair(c0 + at <= last ? y.x : 0.f, c0 + at + 1 <= last ? y.y : 0.f);
+                }
             }
             if (!is_p) {
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(A + j * XP + c0 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                for (int i = 0; i < 8; i += 2) *reinterpret_cast<ulonglong2*>(A + j * XP + c0 + 2 * i) = make_ulonglong2(x[i], x[i + 1]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t hi[4], lo[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], hi[e], lo[e]);
+                    for (int e = 0; e < 4; ++e) split_pair(x[4 * i + e], hi[e], lo[e]);
                     const int at16 = j * 128 + (((c0 / 8 + i) ^ (j & 7)) << 4);
                     *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                     *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -348,21 +357,20 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
     uint8_t* const t_at = work + PREP_T + ts * 128;
     uint32_t w[3][8];
     {
-        float x[16];
+        uint64_t x[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float4 y = *reinterpret_cast<const float4*>(A + ts * XP + tc0 + i), b = *reinterpret_cast<const float4*>(sbeta + tc0 + i);
-            x[i] = tc0 + i <= ts ? y.x * b.x : 0.f;
-            x[i + 1] = tc0 + i + 1 <= ts ? y.y * b.y : 0.f;
-            x[i + 2] = tc0 + i + 2 <= ts ? y.z * b.z : 0.f;
-            x[i + 3] = tc0 + i + 3 <= ts ? y.w * b.w : 0.f;
+            const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(A + ts * XP + tc0 + i), b = *reinterpret_cast<const ulonglong2*>(sbeta + tc0 + i);
+            const float2 u = unpair(mul2(y.x, b.x)), v = unpair(mul2(y.y, b.y));
+            x[i / 2] = pair(tc0 + i <= ts ? u.x : 0.f, tc0 + i + 1 <= ts ? u.y : 0.f);
+            x[i / 2 + 1] = pair(tc0 + i + 2 <= ts ? v.x : 0.f, tc0 + i + 3 <= ts ? v.y : 0.f);
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) split2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1], hi[e], lo[e]);
+            for (int e = 0; e < 4; ++e) split_pair(x[4 * i + e], hi[e], lo[e]);
             const int piece = ((tc0 / 8 + i) ^ (ts & 7)) << 4;
             *reinterpret_cast<uint4*>(t_at + piece) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             *reinterpret_cast<uint4*>(t_at + TILE + piece) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -384,14 +392,9 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
             tc_commit(&done);
         }
         __syncwarp();
-        const float weight = sw[ts];
+        const uint64_t weight = pair(sw[ts], sw[ts]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float u = x[2 * i] * weight, v = x[2 * i + 1] * weight;
-            w[0][i] = pack_bf16(u, v);
-            const float2 hi = unpack_bf16(w[0][i]);
-            split2(u - hi.x, v - hi.y, w[1][i], w[2][i]);
-        }
+        for (int i = 0; i < 8; ++i) split_pair(take_bf16(mul2(x[i], weight), w[0][i]), w[1][i], w[2][i]);
     }
     WAIT(&done, 1);
     tc_fence_after();
@@ -444,7 +447,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
             for (int i = 0; i < 2; ++i) {
                 uint32_t hi[4], lo[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split2(__uint_as_float(r[8 * i + 2 * e]), __uint_as_float(r[8 * i + 2 * e + 1]), hi[e], lo[e]);
+                for (int e = 0; e < 4; ++e) split_pair(pair(r[8 * i + 2 * e], r[8 * i + 2 * e + 1]), hi[e], lo[e]);
                 const int at16 = row * 128 + (((4 * part + 2 * half + i) ^ (row & 7)) << 4);
                 *reinterpret_cast<uint4*>(sm + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 *reinterpret_cast<uint4*>(sm + Out::Y + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -518,12 +521,7 @@ __device__ __forceinline__ void put_split(uint8_t* tile, int lbo, int r, int par
     for (int i = 0; i < 2; ++i) {
         uint32_t h[4], l[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 y = unpair(x[4 * i + e]);
-            h[e] = pack_bf16(y.x, y.y);
-            const float2 z = unpair(add2(x[4 * i + e], pair((h[e] << 16) ^ 0x80000000u, (h[e] & 0xffff0000u) ^ 0x80000000u)));
-            l[e] = pack_bf16(z.x, z.y);
-        }
+        for (int e = 0; e < 4; ++e) split_pair(x[4 * i + e], h[e], l[e]);
         const int piece = 2 * part + i;
         *reinterpret_cast<uint4*>(row + ((piece ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         *reinterpret_cast<uint4*>(row + (W == 32 ? ((piece + 4) ^ (r & 7)) << 4 : lbo + ((piece ^ (r & 7)) << 4))) = make_uint4(l[0], l[1], l[2], l[3]);
@@ -889,14 +887,6 @@ struct Wide {
     static constexpr uint32_t COL_SH = 0, COL_SL = 64, COL_RH = 128, COL_RL = 160, COL_O = 192, COL_X = 256, COL_D = 384, COLS = 512;
     static constexpr uint32_t Y_BYTES = In::BYTES + 2 * TILE;
 };
-
-// A pair of fp32 in two bf16 terms.
-__device__ __forceinline__ void split_pair(uint64_t x, uint32_t& hi, uint32_t& lo) {
-    const float2 y = unpair(x);
-    hi = pack_bf16(y.x, y.y);
-    const float2 z = unpair(add2(x, pair((hi << 16) ^ 0x80000000u, (hi & 0xffff0000u) ^ 0x80000000u)));
-    lo = pack_bf16(z.x, z.y);
-}
 
 __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q,
                                                                            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const DeltaTcParams tp) {
