@@ -91,14 +91,14 @@ constexpr int PREP_THREADS = 256;
 constexpr int XP = 68;                                          // pitch of A and its inverse in shared memory, floats
 constexpr int PREP_A = 0, PREP_SCRATCH = DC * XP * 4;           // behind K and Q; scratch: [32][8] floats of four pairs of warps
 constexpr int PREP_T = 0;                                       // the same room later: T in two terms, then two of the three terms of diag(2^(L_63 - L)) T, then P T
+constexpr uint32_t COL_P = 64;                                  // P in two terms, 32 columns of tensor memory each; Y's sums later
 constexpr int PREP_WORK = PREP_SCRATCH + 4 * 32 * 8 * 4;
 static_assert(PREP_WORK >= 2 * TILE && PREP_WORK % 1024 == 0, "two tiles fit where A and the scratch are");
 
 template <int D>
 struct Prep {
-    // P's high terms take the place of Q's first tile, the low ones that of its second (d = 64 has none: one more), the third term of the weighted T theirs
-    static constexpr int KQ = 2 * TILE * (D / 64), P_LO = D == 128 ? 3 * TILE : KQ + PREP_WORK;
-    static constexpr int META = KQ + PREP_WORK + (D == 128 ? 0 : TILE), SMEM = META + 2 * DC * 4 + 1024;
+    static constexpr int KQ = 2 * TILE * (D / 64), W_LO = TILE;      // the third term of the weighted T takes the place of Q's first tile
+    static constexpr int META = KQ + PREP_WORK, SMEM = META + 2 * DC * 4 + 1024;
 };
 
 template <int D>
@@ -259,26 +259,20 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
             if (!is_p) {
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) *reinterpret_cast<ulonglong2*>(A + j * XP + c0 + 2 * i) = make_ulonglong2(x[i], x[i + 1]);
-            } else {
+            } else {      // an operand in tensor memory, two terms, beside the products
+                uint32_t hi[8], lo[8];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) split_pair(x[4 * i + e], hi[e], lo[e]);
-                    const int at16 = j * 128 + (((c0 / 8 + i) ^ (j & 7)) << 4);
-                    *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                }
+                for (int e = 0; e < 8; ++e) split_pair(x[e], hi[e], lo[e]);
+                tmem_st8(row_addr - 32 * part + COL_P + c0 / 2, hi);
+                tmem_st8(row_addr - 32 * part + COL_P + 32 + c0 / 2, lo);
             }
         }
     } else if (is_p) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at16 = j * 128 + (((4 * part + i) ^ (j & 7)) << 4);
-            *reinterpret_cast<uint4*>(sm + TILE + at16) = make_uint4(0u, 0u, 0u, 0u);
-            *reinterpret_cast<uint4*>(sm + L::P_LO + at16) = make_uint4(0u, 0u, 0u, 0u);
-        }
+        const uint32_t zero[16] = {};
+        tmem_st16(row_addr - 32 * part + COL_P + 16 * part, zero);
+        tmem_st16(row_addr - 32 * part + COL_P + 32 + 16 * part, zero);
     }
+    if (is_p) tc_wait_st();
     tc_fence_before();
     __syncthreads();
     float* scratch = reinterpret_cast<float*>(work + PREP_SCRATCH) + (warp & 3) * 256;      // [rows][8] of this warp's, or this pair's, columns
@@ -379,16 +373,15 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         __syncthreads();
         if (warp == 0 && elect_one()) {
             tc_fence_after();
-            // P T cancels where keys are alike (its rows are differences of P's), so both factors keep two terms.  Rows 64..127 of the operands are P; the
-            // products of the 64 rows before them are not read.
+            // P T cancels where keys are alike (its rows are differences of P's), so both factors keep two terms.  Lanes 64..127 of the operand are P; the
+            // products of the 64 before them are not read.
             constexpr uint32_t ID = idesc_bf16(128, 64, 0, 1);
-            const uint32_t tt = smem_u32(work + PREP_T), p_hi = smem_u32(sm), p_lo = smem_u32(sm + L::P_LO - TILE);
+            const uint32_t tt = smem_u32(work + PREP_T);
 #pragma unroll
-            for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_lo + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID, kk ? 1u : 0u);
+            for (int k = 2; k >= 0; --k)      // P_lo T_hi, P_hi T_lo, P_hi T_hi
 #pragma unroll
-            for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + TILE + kk * 2048, 16, 1024), ID, 1u);
-#pragma unroll
-            for (int kk = 0; kk < DC / 16; ++kk) mma_ss(tb, smem_desc_sw128(p_hi + kk * 32, 16, 1024), smem_desc_sw128(tt + kk * 2048, 16, 1024), ID, 1u);
+                for (int kk = 0; kk < DC / 16; ++kk)
+                    mma_ts(tb, tb + COL_P + (k == 2 ? 32 : 0) + 8 * kk, smem_desc_sw128(tt + (k == 1 ? TILE : 0) + kk * 2048, 16, 1024), ID, k < 2 || kk ? 1u : 0u);
             tc_commit(&done);
         }
         __syncwarp();
@@ -403,14 +396,14 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         const int piece = ((tc0 / 8 + i) ^ (ts & 7)) << 4;
         *reinterpret_cast<uint4*>(t_at + piece) = make_uint4(w[0][4 * i], w[0][4 * i + 1], w[0][4 * i + 2], w[0][4 * i + 3]);
         *reinterpret_cast<uint4*>(t_at + TILE + piece) = make_uint4(w[1][4 * i], w[1][4 * i + 1], w[1][4 * i + 2], w[1][4 * i + 3]);
-        *reinterpret_cast<uint4*>(sm + L::P_LO + ts * 128 + piece) = make_uint4(w[2][4 * i], w[2][4 * i + 1], w[2][4 * i + 2], w[2][4 * i + 3]);
+        *reinterpret_cast<uint4*>(sm + L::W_LO + ts * 128 + piece) = make_uint4(w[2][4 * i], w[2][4 * i + 1], w[2][4 * i + 2], w[2][4 * i + 3]);
     }
     fence_proxy_async_smem();
     __syncthreads();
     if (warp == 0 && elect_one()) {
         tc_fence_after();
         constexpr uint32_t ID = idesc_bf16(128, 64, 1, 1);      // d = 64 has 64 rows, the other half of the product is not read
-        const uint32_t kt = smem_u32(sm), wt = smem_u32(work + PREP_T), w2 = smem_u32(sm + L::P_LO);
+        const uint32_t kt = smem_u32(sm), wt = smem_u32(work + PREP_T), w2 = smem_u32(sm + L::W_LO);
 #pragma unroll
         for (int k = 2; k >= 0; --k)
 #pragma unroll
@@ -437,7 +430,7 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         for (int i = 0; i < 4; ++i)
             *reinterpret_cast<uint4*>(work + PREP_T + j * 128 + (((4 * part + i) ^ (j & 7)) << 4)) = make_uint4(pt[4 * i], pt[4 * i + 1], pt[4 * i + 2], pt[4 * i + 3]);
     }
-    if (row < D) {      // Y where K and P were
+    if (row < D) {      // Y where K and Q were
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             uint32_t r[16];
