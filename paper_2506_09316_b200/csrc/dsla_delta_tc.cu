@@ -4,13 +4,14 @@
 //     A = tril(beta_j D_ji k_j.k_i, -1),   T = (I + A)^-1 diag(beta),   P = scale tril(D_ji q_j.k_i),   Y = K^T diag(2^(L_63 - L)) T
 // a chunk is
 //     R = V - G K S,       O = scale G Q S + (P T) R,       S <- G_63 S + Y R .
-// (4096 tokens, 32 heads of 128: 142 us, the first kernel 50 of them; token by token 1714.)
+// (4096 tokens, 32 heads of 128: 140 us, the first kernel 50 of them; token by token 1714.)
 // Y and P T need no state: a first kernel computes them for all chunks at once (one CTA per chunk and head) into the workspace, a second one walks the
-// chunks of each sequence, two dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v).
+// chunks of each sequence, two dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v), or more columns where there are many heads.
 //
 // Precision.  K, Q, V are bf16 as they come.  What reaches a state is held in two bf16 terms (16 bits of mantissa: S as the operand of K S, R, Y) or three (what
 // Y is made of), with fp32 sums; (I + A)^-1 is fp32.  The state itself stays in fp32 registers and each chunk adds one tensor-core sum to
 // it, with rounding.  P T, which reaches only the bf16 output, has one term.
+// (16 bits: states come out within 5e-6 of exact ones, outputs are as near as their rounding lets them; a third term would be half as many MMAs and operand bytes again.)
 #include <cuda.h>
 
 #include "dsla_delta.cuh"
@@ -470,13 +471,12 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 //   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-// Bound by shared memory and the chain: a chunk takes 2250 cycles, of which copies in (78 KB), operands of 20 MMAs (120 KB) and the rows' own accesses hold its port for about 1850;
-// with W = 64 3400 cycles, 2500 of them held, so half the CTAs of twice the width do more in all once there are enough of them (58K ragged tokens, 32 heads: 1.90 ms with
-// W = 32, 1.73 with W = 64; one sequence of 4096 tokens 143 and 182 us).  Slices of a sequence, the first kernel for one slice under the walk of the slice before, took
-// as long as one after the other (4096 tokens 151 us): both want that port.
-// Where there are more (sequence, head, columns) than SMs, a CTA that is done takes over a block of the grid that has not started, two of them ahead: the next one's
-// loads run under the end of this one's, and barriers and tensor memory are set up once (64 sequences of 64 tokens, 32 heads of 128: 298 us with a CTA for
-// each, 242 so; of 512 tokens 990 and 900).
+// Bound by shared memory and the chain: a chunk takes 2250 cycles, of which copies in (78 KB), operands of 20 MMAs (120 KB) and the rows' own accesses hold its port for about 1850.
+// Slices of a sequence, the first kernel for one slice under the walk of the slice before, took as long as one after the other (4096 tokens 151 us).
+// Where the slabs of 32 columns do not all fit on the device at once, fewer and wider ones do more in all: whole heads for d = 128 (delta_walk_wide_kernel), 64 columns for d = 64
+// (32 heads of 64, 64 sequences of 512 tokens: 766 us with W = 32, 578 with W = 64; 80 heads, one sequence of 2048: 145 and 123).  A CTA that is done then takes over a block
+// of the grid that has not started, two of them ahead: the next one's loads run under the end of this one's, and barriers and tensor memory are set up once (64 sequences of 64
+// tokens, 32 heads of 64: 160 us with a CTA for each, 129 so; of 512 tokens 621 and 578).
 constexpr int WC = 16, ST = 2;      // columns of a thread; stages of loads
 
 template <int D_, int W_>
@@ -873,6 +873,9 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
 //   scale G (Q S)^T + R^T (P T)^T    128 x 64 x 64, two terms, onto what the rows put there; behind it
 // Sixteen row warps, four to a lane quadrant ("parts"): each has 32 columns of d_k of the state in registers; parts 0 and 1 make R of 32 tokens each, 2 and 3 scale Q S and finish
 // the outputs of the chunk before.  V comes transposed through ldmatrix in the fragment layout that R is then stored in, outputs leave through stmatrix.
+// K S is multiplied ahead of Q S, so that R is made under the latter, and the state's columns in two halves, so that half of them are split into terms under the other half's product.
+// Bound by the chain, 3750 cycles a chunk, with HBM at 5 TB/s and the tensor pipe 54 % busy behind it (58K ragged tokens, 32 heads, both kernels: 1.90 ms in slabs of 32 columns, 1.59 in slabs of
+// 64, 1.29 so; 40 heads, one sequence of 2048 tokens, 40 CTAs instead of 160: 133 us in slabs of 32, 113 so).
 struct Wide {
     using In = Chunk<128>;
     static constexpr int D = 128, W = 128, ROW_WARPS = 16, THREADS = 32 * (ROW_WARPS + 2);
