@@ -85,7 +85,7 @@ __device__ __forceinline__ void split_pair(uint64_t x, uint32_t& hi, uint32_t& l
 // Eight warps, two to a lane quadrant (columns 0..31 and 32..63).  [K; Q] K^T is one MMA of 128 rows; quadrants 0, 1 turn its upper half into A, 2, 3 its lower half
 // into P.  (I + A)^-1 in fp32, in A's place: the eight diagonal blocks of 8 by substitution, one column per thread, then three times
 //     [a 0; b c]^-1 = [a^-1 0; -c^-1 b a^-1 c^-1]
-// for pairs of blocks of 8, 16 and 32, columns eight to a warp, as TF32 products of two terms each (22 bits).  Then P T and Y are MMAs, one after the other through
+// for pairs of blocks of 8, 16 and 32, as TF32 products of two terms each (22 bits); a warp takes 16 columns, so that the other factor is split into terms half as often.  Then P T and Y are MMAs, one after the other through
 // the same tiles: 56 KB and 64 registers a thread keep four CTAs on an SM.  4096 tokens of 32 heads: 52 us with 75 KB and three CTAs; 110 us with a substitution over
 // all 64 rows by 64 threads, 2016 steps of the chain each, and T written two bytes at a time.
 constexpr int PREP_THREADS = 256;
@@ -313,38 +313,42 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         }
         __syncwarp();
         // the pair of them (rows 8..15 of the fragments are whatever lies below)
-        float f[4];
-        product<1>(f, A + (b0 + 8) * XP + b0, XP, 1, A + b0 * XP + b0, XP, 1, 0, 1, lane);
-        *reinterpret_cast<float2*>(scratch + fr_ * 8 + 2 * fq) = make_float2(-f[0], -f[1]);
+        float f[1][4];
+        products<1, 1, false>(f, A + (b0 + 8) * XP + b0, XP, 1, A + b0 * XP + b0, XP, 1, 0, 0, 1, lane);
+        *reinterpret_cast<float2*>(scratch + fr_ * 8 + 2 * fq) = make_float2(-f[0][0], -f[0][1]);
         __syncwarp();
-        product<1>(f, A + (b0 + 8) * XP + b0 + 8, XP, 1, scratch, 8, 1, 0, 1, lane);
-        *reinterpret_cast<float2*>(A + (b0 + 8 + fr_) * XP + b0 + 2 * fq) = make_float2(f[0], f[1]);
+        products<1, 1, false>(f, A + (b0 + 8) * XP + b0 + 8, XP, 1, scratch, 8, 1, 0, 0, 1, lane);
+        *reinterpret_cast<float2*>(A + (b0 + 8 + fr_) * XP + b0 + 2 * fq) = make_float2(f[0][0], f[0][1]);
+    }
+    __syncthreads();
+    float* const cells = reinterpret_cast<float*>(work + PREP_SCRATCH) + (warp & 1) * 512;      // two blocks of [rows][8]
+    if (warp < 2) {      // pairs of blocks of 16
+        const int c0 = 32 * warp, r0 = c0 + 16;
+        float f[2][4];
+        products<2, 2, false>(f, A + r0 * XP + c0, XP, 1, A + c0 * XP + c0, XP, 1, 8, 0, 2, lane);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) put_fragment(cells + 256 * n, 8, f[n], -1.f, lane);
+        __syncwarp();
+        products<2, 2, false>(f, A + r0 * XP + r0, XP, 1, cells, 8, 1, 256, 0, 2, lane);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) put_fragment(A + r0 * XP + c0 + 8 * n, XP, f[n], 1.f, lane);
     }
     __syncthreads();
     {
-        // pairs of blocks of 16: warp = pair and 8 columns
-        const int r0 = 32 * ((warp >> 1) & 1) + 16, c0 = r0 - 16, n0 = 8 * (warp & 1);
-        float f[4];
+        // the pair of blocks of 32: warp = 16 rows and 16 columns
+        const int m0 = 16 * (warp >> 1), n0 = 16 * (warp & 1);
+        float f[2][4];
         if (warp < 4) {
-            product<2>(f, A + r0 * XP + c0, XP, 1, A + c0 * XP + c0 + n0, XP, 1, n0 / 8, 2, lane);
-            put_fragment(scratch, 8, f, -1.f, lane);
+            products<4, 2, false>(f, A + (32 + m0) * XP, XP, 1, A + n0, XP, 1, 8, n0 / 8, 4, lane);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) put_fragment(cells + 256 * n + m0 * 8, 8, f[n], -1.f, lane);
         }
         __syncthreads();
         if (warp < 4) {
-            product<2>(f, A + r0 * XP + r0, XP, 1, scratch, 8, 1, 0, 2, lane);
-            put_fragment(A + r0 * XP + c0 + n0, XP, f, 1.f, lane);
+            products<4, 2, false>(f, A + (32 + m0) * XP + 32, XP, 1, cells, 8, 1, 256, 0, m0 ? 4 : 2, lane);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) put_fragment(A + (32 + m0) * XP + n0 + 8 * n, XP, f[n], 1.f, lane);
         }
-    }
-    __syncthreads();
-    {
-        // the pair of blocks of 32: warp = 16 rows and 8 columns
-        const int m0 = 16 * part, n0 = 8 * quad;
-        float f[4];
-        product<4>(f, A + (32 + m0) * XP, XP, 1, A + n0, XP, 1, quad, 4, lane);
-        put_fragment(scratch + m0 * 8, 8, f, -1.f, lane);
-        __syncthreads();
-        product<4>(f, A + (32 + m0) * XP + 32, XP, 1, scratch, 8, 1, 0, part ? 4 : 2, lane);
-        put_fragment(A + (32 + m0) * XP + n0, XP, f, 1.f, lane);
     }
     __syncthreads();
     // T = inverse diag(beta) into tiles, then with its rows weighted; thread = 16 columns of a row
