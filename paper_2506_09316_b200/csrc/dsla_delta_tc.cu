@@ -610,8 +610,8 @@ __device__ __forceinline__ bool walk_set_up(WalkShared& sh, const DeltaParams& p
 
 // The loading warp.
 template <class L>
-__device__ __forceinline__ void walk_load(WalkShared& sh, const CUtensorMap& map_k, const CUtensorMap& map_q, const CUtensorMap& map_v, const DeltaTcParams& tp, uint8_t* sm, bool sorted,
-                                          int lane) {
+__device__ __forceinline__ void walk_load(WalkShared& sh, const CUtensorMap& map_k, const CUtensorMap& map_q, const CUtensorMap& map_v, const CUtensorMap& map_o,
+                                          const DeltaTcParams& tp, uint8_t* sm, bool sorted, int lane) {
     using In = typename L::In;
     constexpr bool MORE = L::W > 32;      // slabs of 32 columns are for grids that fit on the device at once
     constexpr int D = L::D, W = L::W, SLABS = D / W;
@@ -639,7 +639,8 @@ __device__ __forceinline__ void walk_load(WalkShared& sh, const CUtensorMap& map
         if (x.live && p.use_initial_state)      // rows of the state, on their way before they are asked for
             for (int i = lane; i < D; i += 32)
                 asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p.state + (((size_t)x.slot * p.H + x.h) * D + i) * D + x.column), "n"(W * 4) : "memory");
-        if (lane == 0) {
+        if (lane == 0 && x.chunks > 0) {
+            if (cc == 0) prefetch_tensormap(&map_o);
             const int hq = x.h / p.group;
             for (int c = 0; c < x.chunks && !*abortp; ++c, ++cc) {
                 const int st = cc % ST, t = x.t_begin + c * DC;
@@ -685,8 +686,7 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     const uint32_t tb = sh.tmem_base;
 
     if (warp == LOAD_WARP) {
-        if (lane == 0) prefetch_tensormap(&map_o);
-        walk_load<L>(sh, map_k, map_q, map_v, tp, sm, sorted, lane);
+        walk_load<L>(sh, map_k, map_q, map_v, map_o, tp, sm, sorted, lane);
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
         constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1);
@@ -903,8 +903,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
     const uint32_t tb = sh.tmem_base;
 
     if (warp == LOAD_WARP) {
-        if (lane == 0) prefetch_tensormap(&map_o);
-        walk_load<L>(sh, map_k, map_q, map_v, tp, sm, sorted, lane);
+        walk_load<L>(sh, map_k, map_q, map_v, map_o, tp, sm, sorted, lane);
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm);
         constexpr uint32_t ID = idesc_bf16(128, 64, 0, 0);

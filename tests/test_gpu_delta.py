@@ -455,3 +455,33 @@ def test_many_blocks_on_two_streams_and_in_graphs(impl, dtype, d):
 
     for run in (eager, replayed, eager, replayed):
         check(run)
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+def test_far_offsets_with_many_heads(impl, dtype, d):
+    """More heads than SMs hold in slabs of 32 columns: tokens and slots whose element offsets pass 32 bits."""
+    dsla = _dsla()
+    H, n = 40 * 128 // d, 150
+    far, slots = 430_000, 3400
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    tail = _draw(n, H, 1, d, dtype, 12)
+    whole = [torch.zeros((far + n,) + x.shape[1:], dtype=x.dtype, device="cuda") for x in tail]
+    for x, y in zip(whole, tail):
+        x[far:] = y
+    assert whole[2].numel() > 1 << 31
+    st, small = dsla.dsla_state_alloc_n(slots * 128 // d, 1, H, d, d), dsla.dsla_state_alloc_n(1, 1, H, d, d)
+    assert st.tensor.numel() > 1 << 31
+    st.tensor[-2:] = 0.5
+    small.tensor.fill_(0.5)
+    got = dsla.dsla_delta_prefill(*whole, st, o=torch.zeros_like(whole[2]), cu_seqlens=torch.tensor([far, far + n], dtype=torch.int32, device="cuda"), max_seqlen=n, impl=impl,
+                                  slots=torch.tensor([st.tensor.shape[0] - 1], dtype=torch.int32, device="cuda"), use_initial_state=True)
+    want = dsla.dsla_delta_prefill(*tail, small, impl=impl, use_initial_state=True)
+    assert torch.equal(got[far:], want) and torch.equal(st.tensor[-1], small.tensor[0]) and not bool(got[:far].any()) and bool((st.tensor[-2] == 0.5).all())
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+@pytest.mark.parametrize("lens", [[1], [64], [65, 31, 33, 63], [32, 96, 95, 97, 160]])
+def test_ends_inside_a_chunk_with_many_heads(impl, dtype, d, lens):
+    """Ends on, before and behind the boundaries of 32 tokens, at which outputs leave another way; rows of one sequence border on the next one's."""
+    _check(lens, 80, 2, d, dtype, impl, seed=31, resume=True)
