@@ -485,3 +485,37 @@ def test_far_offsets_with_many_heads(impl, dtype, d):
 def test_ends_inside_a_chunk_with_many_heads(impl, dtype, d, lens):
     """Ends on, before and behind the boundaries of 32 tokens, at which outputs leave another way; rows of one sequence border on the next one's."""
     _check(lens, 80, 2, d, dtype, impl, seed=31, resume=True)
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+@pytest.mark.parametrize("gate,beta", [(0.0, "mixed"), ("tiny", "mixed"), ("mixed", 0.0), (1.0, 2.0), (1.0, 1.0)])
+def test_gates_and_repeated_keys_with_many_heads(impl, dtype, d, gate, beta):
+    def same(q, k, v, g, b):
+        if gate == beta:      # one key over and over, then tokens without one
+            k[1:] = k[:1]
+            k[40:50] = 0
+    _check([140, 10], 80, 1, d, dtype, impl, seed=32, gate=gate, beta=beta, resume=True, edit=same)
+
+
+@pytest.mark.parametrize("impl,dtype,d", CHUNKED)
+def test_rows_that_belong_to_no_sequence_with_many_heads(impl, dtype, d):
+    """Rows before the first and behind the last sequence hold NaN and infinities, and stay as they are; so do the slots of no sequence."""
+    dsla = _dsla()
+    H = 80
+    x = _draw(300, H, 1, d, dtype, 33)
+    cu = torch.tensor([37, 37, 137, 170, 265], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([6, 1, 4, 2], dtype=torch.int32, device="cuda")
+    st = dsla.dsla_state_alloc_n(8, 1, H, d, d)
+    out = []
+    for bad in (0.0, float("nan"), float("inf")):
+        y = [z.clone() for z in x]
+        for z in y:
+            z[:37] = bad
+            z[265:] = bad
+        st.tensor.fill_(0.25)
+        o = torch.full_like(y[2], 5.0)
+        dsla.dsla_delta_prefill(*y, st, o=o, cu_seqlens=cu, slots=slots, max_seqlen=100, impl=impl, use_initial_state=True)
+        assert bool((o[:37] == 5).all()) and bool((o[265:] == 5).all()) and bool(torch.isfinite(o).all())
+        assert all(bool((st.tensor[n] == 0.25).all()) for n in (0, 3, 5, 6, 7)) and dsla.dsla_state_last_error(st) == dsla.DSLA_OK
+        out.append((o, st.tensor.clone()))
+    assert all(torch.equal(out[0][0], o) and torch.equal(out[0][1], s) for o, s in out[1:])
