@@ -4,7 +4,7 @@
 //     A = tril(beta_j D_ji k_j.k_i, -1),   T = (I + A)^-1 diag(beta),   P = scale tril(D_ji q_j.k_i),   Y = K^T diag(2^(L_63 - L)) T
 // a chunk is
 //     R = V - G K S,       O = scale G Q S + (P T) R,       S <- G_63 S + Y R .
-// (4096 tokens, 32 heads of 128: 140 us, the first kernel 50 of them; token by token 1714.)
+// (4096 tokens, 32 heads of 128: 136 us, the first kernel 48 of them; token by token 1714.)
 // Y and P T need no state: a first kernel computes them for all chunks at once (one CTA per chunk and head) into the workspace, a second one walks the
 // chunks of each sequence, two dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v), or more columns where there are many heads.
 //
@@ -471,11 +471,11 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 // Warps 0..7 work on rows, two for each lane quadrant (16 columns each), 8 issues the MMAs, 9 loads.  (Issued by a row warp the MMAs hold up that warp's rows: 2750
 // cycles per chunk instead of 2450.)  With W = 32 columns of d_v, per chunk:
 //   [K; Q] [S_hi | S_lo]          128 x 64 x d    lanes 0..63 K S, 64..127 Q S
-//   (Y_hi + Y_lo) [R_hi | R_lo]   128 x 64 x 64   lanes d_k; on the chain
+//   Y_hi [R_hi | R_lo] + Y_lo R_hi   128 x 64 x 64   lanes d_k; on the chain (low by low left out: 2^-18; 4096 tokens 130.8 to 129.4 us)
 //   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-// Bound by shared memory and the chain: a chunk takes 2250 cycles, of which copies in (78 KB), operands of 20 MMAs (120 KB) and the rows' own accesses hold its port for about 1850.
+// Bound by shared memory and the chain: a chunk takes 2200 cycles, of which copies in (78 KB), operands of 20 MMAs (116 KB) and the rows' own accesses hold its port for about 1820.
 // Slices of a sequence, the first kernel for one slice under the walk of the slice before, took as long as one after the other (4096 tokens 151 us).
 // Where the slabs of 32 columns do not all fit on the device at once, fewer and wider ones do more in all: whole heads for d = 128 (delta_walk_wide_kernel), 64 columns for d = 64
 // (32 heads of 64, 64 sequences of 512 tokens: 766 us with W = 32, 578 with W = 64; 80 heads, one sequence of 2048: 145 and 123).  A CTA that is done then takes over a block
@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
         walk_load<L>(sh, map_k, map_q, map_v, map_o, tp, sm, sorted, lane);
     } else if (warp == MMA_WARP) {
         const uint32_t base = smem_u32(sm), s_at = base + L::OFF_S, r_at = base + L::OFF_R;
-        constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1);
+        constexpr uint32_t ID = idesc_bf16(128, 2 * W, 0, 1), ID_HI = idesc_bf16(128, W, 0, 1);
         int c = 0;      // chunks of all items
         for (int it = 0;; ++it) {
             item_wait<L::THREADS>(PUBLISHED + (it & 1));
@@ -717,10 +717,10 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 1; k >= 0; --k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
+                    for (int k = 0; k < 2; ++k)      // d = 64: rows 64..127 are what lies behind, their lanes are not read
 #pragma unroll
                         for (int kk = 0; kk < DC / 16; ++kk)
-                            mma_ss(tb + L::COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, !k || kk ? 1u : 0u);
+                            mma_ss(tb + L::COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), k ? ID_HI : ID, k || kk ? 1u : 0u);
                     tc_commit(&d_full);
 #pragma unroll
                     for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
