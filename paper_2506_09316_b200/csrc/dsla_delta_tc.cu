@@ -4,14 +4,13 @@
 //     A = tril(beta_j D_ji k_j.k_i, -1),   T = (I + A)^-1 diag(beta),   P = scale tril(D_ji q_j.k_i),   Y = K^T diag(2^(L_63 - L)) T
 // a chunk is
 //     R = V - G K S,       O = scale G Q S + (P T) R,       S <- G_63 S + Y R .
-// (4096 tokens, 32 heads of 128: 136 us, the first kernel 48 of them; token by token 1714.)
 // Y and P T need no state: a first kernel computes them for all chunks at once (one CTA per chunk and head) into the workspace, a second one walks the
 // chunks of each sequence, two dependent products to a chunk, one CTA per (sequence, head, 32 columns of d_v), or more columns where there are many heads.
 //
-// Precision.  K, Q, V are bf16 as they come.  What reaches a state is held in two bf16 terms (16 bits of mantissa: S as the operand of K S, R, Y) or three (what
-// Y is made of), with fp32 sums; (I + A)^-1 is fp32.  The state itself stays in fp32 registers and each chunk adds one tensor-core sum to
-// it, with rounding.  P T, which reaches only the bf16 output, has one term.
-// (16 bits: states come out within 5e-6 of exact ones, outputs are as near as their rounding lets them; a third term would be half as many MMAs and operand bytes again.)
+// Precision.  K, Q, V are bf16 as they come.  What reaches a state or an output is held in two bf16 terms (16 bits of mantissa: S as the operand of K S and Q S, R, Y, P T and
+// its factors) or three (what Y is made of), with fp32 sums; (I + A)^-1 is fp32.  The state itself stays in fp32 registers and each chunk adds one tensor-core sum to
+// it, with rounding.  So outputs are off by their own rounding and by less than 3e-6 of the size of their summands (P T in one term: 1.6e-3 of it, as much as the rounding; a
+// second term for it costs 3 to 4 % of time); states by up to 1.7e-5 of their head's largest value, which is the rounding of Y (a third term would be half as many MMAs and operand bytes again).
 #include <cuda.h>
 
 #include "dsla_delta.cuh"
@@ -28,8 +27,9 @@ namespace {
 
 constexpr int DC = 64;                          // tokens per chunk
 constexpr int TILE = DC * 128;                  // bytes of 64 rows of 64 bf16
-// A chunk in the workspace: Y's high terms and its low terms, each [d][64] bf16, and P T [64][64] bf16, as the MMAs read them (128-byte swizzle), then scale G
-// and G, each [64] fp32.
+// A chunk in the workspace: Y's high terms and its low terms, each [d][64] bf16, as the MMAs read them (128-byte swizzle); P T, [64][64] bf16, swizzled alike; then the low terms of P T's
+// diagonal, [64] bf16, 128 bytes of nothing, and G, [64] fp32.  P T has nothing above its diagonal, so its low terms fill that half, turned by 180 degrees: row r holds the high terms
+// (r, c) where c <= r, and the low terms (63 - r, 63 - c) where c > r.
 template <int D>
 struct Chunk {
     static constexpr int Y = D * 128, PT = 2 * Y, META = PT + TILE, BYTES = META + 2 * DC * 4;
@@ -65,6 +65,27 @@ __device__ __forceinline__ void find_sequence(const DeltaTcParams& tp, int n, in
         t_begin = n * tp.p.T;
         len = tp.p.T;
         first = n * tp.chunks;
+    }
+}
+
+// Columns c and c + 1, c even, of row j of a triangle, its diagonal included: which halves of the word belong to it.
+__device__ __forceinline__ uint32_t triangle_mask(int j, int c) { return j > c ? 0xffffffffu : j == c ? 0xffffu : 0u; }
+// N pieces of eight columns, from piece `first` on, of row j of P T out of a chunk in shared memory: high and low terms.
+template <int N>
+__device__ __forceinline__ void take_pt(const uint8_t* pt, const uint8_t* diagonal, int j, int first, uint32_t (&hi)[4 * N], uint32_t (&lo)[4 * N]) {
+    const uint32_t corner = 0x10001u * reinterpret_cast<const uint16_t*>(diagonal)[j];
+    const int m = 63 - j;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int piece = first + i;
+        const uint4 x = *reinterpret_cast<const uint4*>(pt + j * 128 + ((piece ^ (j & 7)) << 4)), y = *reinterpret_cast<const uint4*>(pt + m * 128 + (((7 - piece) ^ (m & 7)) << 4));
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.w, y.z, y.y, y.x};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t with = triangle_mask(j, 8 * piece + 2 * e), below = triangle_mask(j - 1, 8 * piece + 2 * e), turned = __byte_perm(ys[e], 0u, 0x1032);
+            hi[4 * i + e] = xs[e] & with;
+            lo[4 * i + e] = (turned & below) | (corner & with & ~below);
+        }
     }
 }
 
@@ -187,14 +208,13 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * lane + i;
-            const float hi = (float)run[i], G = ex2(hi);
+            const float hi = (float)run[i];
             mhi[j] = -hi;      // minus the sums: differences are additions
             mlo[j] = (float)(hi - run[i]);
             sbeta[j] = beta[i];
             sw[j] = ex2((float)(last - run[i]));
             if (j < 32) sleft[j] = ex2((float)(middle - run[i]));
-            meta[j] = G * p.scale;
-            meta[DC + j] = G;
+            meta[DC + j] = ex2(hi);
         }
     }
     tc_fence_before();
@@ -417,23 +437,43 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
         tc_commit(&done);
     }
     __syncwarp();
-    uint32_t pt[16];
-    if (is_p) {
+    uint32_t pt[2][16];      // P T, high and low terms (nothing right of the diagonal's block of 32)
+    const bool packs = is_p && upper >= part, on_diagonal = is_p && upper == part;
+    if (packs) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             uint32_t r[16];
             tmem_ld16(row_addr + 16 * half, r);
             tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pt[8 * half + i] = pack_bf16(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+            for (int i = 0; i < 8; ++i) split_pair(pair(r[2 * i], r[2 * i + 1]), pt[0][8 * half + i], pt[1][8 * half + i]);
         }
     }
     WAIT(&done, 0);
     tc_fence_after();
-    if (is_p) {         // P T where T was
+    if (packs) {         // into one tile, where T was; the pieces that hold both, those of the diagonal, by way of [64][8] of each behind it
+        uint8_t *const tile = work + PREP_T, *const edge = work + 2 * TILE;
+        const int mine = j >> 3, m = 63 - j;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(work + PREP_T + j * 128 + (((4 * part + i) ^ (j & 7)) << 4)) = make_uint4(pt[4 * i], pt[4 * i + 1], pt[4 * i + 2], pt[4 * i + 3]);
+        for (int i = 0; i < 4; ++i) {
+            const int piece = 4 * part + i;
+            const uint32_t* l = pt[1] + 4 * i;
+            if (piece <= mine) {
+                uint8_t* const at = piece < mine ? tile + j * 128 + ((piece ^ (j & 7)) << 4) : edge + j * 16;
+                uint8_t* const turned = piece < mine ? tile + m * 128 + (((7 - piece) ^ (m & 7)) << 4) : edge + (DC + j) * 16;
+                *reinterpret_cast<uint4*>(at) = make_uint4(pt[0][4 * i], pt[0][4 * i + 1], pt[0][4 * i + 2], pt[0][4 * i + 3]);
+                *reinterpret_cast<uint4*>(turned) = make_uint4(__byte_perm(l[3], 0u, 0x1032), __byte_perm(l[2], 0u, 0x1032), __byte_perm(l[1], 0u, 0x1032), __byte_perm(l[0], 0u, 0x1032));
+            }
+        }
+        if (on_diagonal) {
+            asm volatile("bar.sync 1, 64;" ::: "memory");      // two warps, a thread to a row
+            const uint4 x = *reinterpret_cast<const uint4*>(edge + j * 16), y = *reinterpret_cast<const uint4*>(edge + (DC + m) * 16);
+            const int e = j & 7;
+            const uint32_t k0 = triangle_mask(e, 0), k1 = triangle_mask(e, 2), k2 = triangle_mask(e, 4), k3 = triangle_mask(e, 6);
+            *reinterpret_cast<uint4*>(tile + j * 128 + ((mine ^ e) << 4)) =
+                make_uint4((x.x & k0) | (y.x & ~k0), (x.y & k1) | (y.y & ~k1), (x.z & k2) | (y.z & ~k2), (x.w & k3) | (y.w & ~k3));
+            reinterpret_cast<uint16_t*>(sm + L::META)[j] = reinterpret_cast<const uint16_t*>(edge + (DC + j) * 16)[7 - e];
+        }
     }
     if (row < D) {      // Y where K and Q were
 #pragma unroll
@@ -471,11 +511,11 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 // Warps 0..7 work on rows, two for each lane quadrant (16 columns each), 8 issues the MMAs, 9 loads.  (Issued by a row warp the MMAs hold up that warp's rows: 2750
 // cycles per chunk instead of 2450.)  With W = 32 columns of d_v, per chunk:
 //   [K; Q] [S_hi | S_lo]          128 x 64 x d    lanes 0..63 K S, 64..127 Q S
-//   Y_hi [R_hi | R_lo] + Y_lo R_hi   128 x 64 x 64   lanes d_k; on the chain (low by low left out: 2^-18; 4096 tokens 130.8 to 129.4 us)
-//   P T [R_hi | R_lo]             128 x 64 x 64   lanes 64..127, behind it
+//   Y_hi [R_hi | R_lo] + Y_lo R_hi   128 x 64 x 64   lanes d_k; on the chain (low by low left out: 2^-16 at most)
+//   PT_hi [R_hi | R_lo] + PT_lo R_hi   the same, lanes 64..127, P T out of tensor memory; behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
-// runs.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-// Bound by shared memory and the chain: a chunk takes 2200 cycles, of which copies in (78 KB), operands of 20 MMAs (116 KB) and the rows' own accesses hold its port for about 1820.
+// runs, and take its P T apart into tensor memory.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
+// Bound by shared memory and the chain: a chunk takes 2300 cycles; copies in (78 KB), operands of 24 MMAs (104 KB) and the rows' own accesses hold its port for most of them.
 // Slices of a sequence, the first kernel for one slice under the walk of the slice before, took as long as one after the other (4096 tokens 151 us).
 // Where the slabs of 32 columns do not all fit on the device at once, fewer and wider ones do more in all: whole heads for d = 128 (delta_walk_wide_kernel), 64 columns for d = 64
 // (32 heads of 64, 64 sequences of 512 tokens: 766 us with W = 32, 578 with W = 64; 80 heads, one sequence of 2048: 145 and 123).  A CTA that is done then takes over a block
@@ -492,7 +532,7 @@ struct Walk {
     // Operands of W columns in two terms: rows of [32 high | 32 low], or a tile of 64 high and one of 64 low columns behind each other.
     static constexpr int S_BYTES = D * 4 * W, R_BYTES = DC * 4 * W, S_LBO = D * 128, R_LBO = TILE;
     static constexpr int OFF_S = OFF_Y + ST * Y_STAGE, OFF_R = OFF_S + S_BYTES, OFF_O = OFF_R + R_BYTES, SMEM = OFF_O + 2 * PARTS * 1024 + 1024;
-    static constexpr uint32_t COL_X = 0, COL_D = 2 * W, COL_O = 4 * W, COLS = W == 32 ? 256 : 512;
+    static constexpr uint32_t COL_X = 0, COL_D = 2 * W, COL_O = 4 * W, COL_P = 6 * W, COLS = W == 32 ? 256 : 512;      // (P T: 32 columns for each term)
     static constexpr uint32_t Y_BYTES = In::BYTES + DC * W * 2;
 };
 
@@ -557,7 +597,7 @@ constexpr int PUBLISHED = 3, READ = 5;
 
 struct WalkShared {
     __align__(16) uint8_t answer[16];
-    uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, o_free, answered;
+    uint64_t kq_full[ST], kq_empty[ST], y_full[ST], y_empty[ST], x_full, d_full, o_full, answered;
     uint64_t q_full, d2_full;      // a whole head to a CTA: Q S, and the second half of the state's columns
     Item items[2];
     uint8_t order[128];
@@ -581,7 +621,6 @@ __device__ __forceinline__ bool walk_set_up(WalkShared& sh, const DeltaParams& p
         mbar_init(&sh.d2_full, 1);
         mbar_init(&sh.d_full, 1);
         mbar_init(&sh.o_full, 1);
-        mbar_init(&sh.o_free, L::ROW_WARPS / 2);
         sh.abort_flag = 0;
         fence_barrier_init();
     }
@@ -676,7 +715,7 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
     extern __shared__ uint8_t smem_raw[];
     __shared__ WalkShared sh;
     uint64_t *kq_full = sh.kq_full, *kq_empty = sh.kq_empty, *y_full = sh.y_full, *y_empty = sh.y_empty;
-    uint64_t &x_full = sh.x_full, &d_full = sh.d_full, &o_full = sh.o_full, &o_free = sh.o_free;
+    uint64_t &x_full = sh.x_full, &d_full = sh.d_full, &o_full = sh.o_full;
     Item* items = sh.items;
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
     const DeltaParams& p = tp.p;
@@ -712,7 +751,6 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
                 }
                 __syncwarp();
                 WAIT(&y_full[st], (c / ST) & 1);
-                if (c > 0) WAIT(&o_free, (c - 1) & 1);
                 rows_wait<2, L::ROW_WARPS / 2>();
                 tc_fence_after();
                 if (elect_one()) {
@@ -722,9 +760,16 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
                         for (int kk = 0; kk < DC / 16; ++kk)
                             mma_ss(tb + L::COL_D, smem_desc_sw128(y + k * In::Y + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), k ? ID_HI : ID, k || kk ? 1u : 0u);
                     tc_commit(&d_full);
+                }
+                __syncwarp();
+                rows_wait<7, L::ROW_WARPS / 2>();      // P T is there, and the sums of the chunk before have been read
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < DC / 16; ++kk)      // P T in rows 64..127; the rows before it are Y's
-                        mma_ss(tb + L::COL_O, smem_desc_sw128(y + In::PT - TILE + kk * 32, 16, 1024), smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), ID, kk ? 1u : 0u);
+                    for (int k = 0; k < 2; ++k)      // P T in lanes 64..127; what the lanes before them give is not read
+#pragma unroll
+                        for (int kk = 0; kk < DC / 16; ++kk)
+                            mma_ts(tb + L::COL_O, tb + L::COL_P + 32 * k + 8 * kk, smem_desc_sw128(r_at + kk * 2048, L::R_LBO, 1024), k ? ID_HI : ID, k || kk ? 1u : 0u);
                     tc_commit(&o_full);
                     tc_commit(&y_empty[st]);
                 }
@@ -752,8 +797,6 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
             tmem_ld16(lane_addr + L::COL_O + W, b);
             tc_wait_ld();
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&o_free);
             uint32_t z[WC / 2];
 #pragma unroll
             for (int i = 0; i < WC / 2; ++i) {
@@ -833,7 +876,23 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
                     if (c > 0) outputs(x, c - 1);
                     WAIT_HOT(&y_full[st], (cc / ST) & 1);
                     last = meta[2 * DC - 1];
-                    const float G = meta[j];
+                    const float G = meta[DC + j] * p.scale;
+                    {
+                        constexpr int WORDS = 32 / L::PARTS;
+                        uint32_t hi[WORDS], lo[WORDS];
+                        take_pt<WORDS / 4>(stage + In::PT, stage + In::META, j, WORDS / 4 * part, hi, lo);
+                        const uint32_t to = tb + ((uint32_t)(32 * quad) << 16) + L::COL_P + WORDS * part;
+                        if constexpr (WORDS == 16) {
+                            tmem_st16(to, hi);
+                            tmem_st16(to + 32, lo);
+                        } else {
+                            tmem_st8(to, hi);
+                            tmem_st8(to + 32, lo);
+                        }
+                        tc_wait_st();
+                        tc_fence_before();
+                        rows_arrive<7, L::ROW_WARPS / 2>();
+                    }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&y_empty[st]);
                     WAIT_HOT(&x_full, cc & 1);
@@ -873,17 +932,17 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
 // The walk with a whole head of d = 128 to a CTA, everything turned over: lanes of TMEM are columns of d_v.  S^T and R^T are A operands in tensor memory, two terms each, so only
 // K, Q, Y and P T, the B operands, pass through shared memory, once for all 128 columns:
 //   S^T [K; Q]^T            128 x 128 x 128, two terms    columns 0..63 (K S)^T, 64..127 (Q S)^T
-//   R^T Y^T                 128 x 128 x 64, three products of terms (low by low left out: 2^-18); on the chain
-//   scale G (Q S)^T + R^T (P T)^T    128 x 64 x 64, two terms, onto what the rows put there; behind it
-// Sixteen row warps, four to a lane quadrant ("parts"): each has 32 columns of d_k of the state in registers; parts 0 and 1 make R of 32 tokens each, 2 and 3 scale Q S and finish
-// the outputs of the chunk before.  V comes transposed through ldmatrix in the fragment layout that R is then stored in, outputs leave through stmatrix.
+//   R^T Y^T                 128 x 128 x 64, three products of terms (low by low left out: 2^-16 at most); on the chain
+//   scale G (Q S)^T + R^T (P T)^T    128 x 64 x 64, three products of terms, onto what the rows put there; behind it
+// Sixteen row warps, four to a lane quadrant ("parts"): each has 32 columns of d_k of the state in registers; parts 0 and 1 make R of 32 tokens each, 2 and 3 take P T apart into
+// two tiles, scale Q S and finish the outputs of the chunk before.  V comes transposed through ldmatrix in the fragment layout that R is then stored in, outputs leave through stmatrix.
 // K S is multiplied ahead of Q S, so that R is made under the latter, and the state's columns in two halves, so that half of them are split into terms under the other half's product.
 // Bound by the chain, 3750 cycles a chunk, with HBM at 5 TB/s and the tensor pipe 54 % busy behind it (58K ragged tokens, 32 heads, both kernels: 1.90 ms in slabs of 32 columns, 1.59 in slabs of
 // 64, 1.29 so; 40 heads, one sequence of 2048 tokens, 40 CTAs instead of 160: 133 us in slabs of 32, 113 so).
 struct Wide {
     using In = Chunk<128>;
     static constexpr int D = 128, W = 128, ROW_WARPS = 16, THREADS = 32 * (ROW_WARPS + 2);
-    static constexpr int KQ = 4 * TILE, V = (In::BYTES + 1023) & ~1023, Y_STAGE = V + 2 * TILE, OFF_Y = ST * KQ, OFF_O = OFF_Y + ST * Y_STAGE, SMEM = OFF_O + 8 * 2048 + 1024;
+    static constexpr int KQ = 4 * TILE, V = (In::BYTES + 1023) & ~1023, Y_STAGE = V + 2 * TILE, OFF_Y = ST * KQ, OFF_PT = OFF_Y + ST * Y_STAGE, OFF_O = OFF_PT + 2 * TILE, SMEM = OFF_O + 8 * 2048 + 1024;
     static constexpr uint32_t COL_SH = 0, COL_SL = 64, COL_RH = 128, COL_RL = 160, COL_O = 192, COL_X = 256, COL_D = 384, COLS = 512;
     static constexpr uint32_t Y_BYTES = In::BYTES + 2 * TILE;
 };
@@ -963,10 +1022,10 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 1; k >= 0; --k)
+                    for (int k = 2; k >= 0; --k)      // R_hi PT_lo, R_lo PT_hi, R_hi PT_hi
 #pragma unroll
                         for (int kk = 0; kk < DC / 16; ++kk)
-                            mma_ts(tb + L::COL_O, tb + (k ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(y + In::PT + kk * 32, 16, 1024), ID, 1u);
+                            mma_ts(tb + L::COL_O, tb + (k == 1 ? L::COL_RL : L::COL_RH) + 8 * kk, smem_desc_sw128(base + L::OFF_PT + (k == 2 ? TILE : 0) + kk * 32, 16, 1024), ID, 1u);
                     tc_commit(&sh.o_full);
                     tc_commit(&sh.y_empty[st]);
                 }
@@ -979,6 +1038,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
         const bool makes_r = part < 2;
         const int tok = 32 * (part & 1);      // this warp's tokens of a chunk: R's, or the outputs'
         uint64_t s[16];                       // S^T: columns 32 part .. of d_k
+        const uint64_t scale = pair(p.scale, p.scale);
         int cc = 0;                           // chunks of all items so far
         uint8_t* o_tile = sm + L::OFF_O + (quad + 4 * (part & 1)) * 2048;      // 32 tokens x 32 columns, rows of 64 bytes, swizzled
         // The outputs of chunk c (parts 2, 3), the latest of all.  Whole rows of 32 tokens leave by a TMA store of this warp, those of a ragged end row by row.
@@ -1098,6 +1158,19 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                     if (c > 0) outputs(x, c - 1);
                     WAIT_HOT(&sh.y_full[st], (cc / ST) & 1);
                     last = meta[2 * DC - 1];
+                    {      // P T as an operand: a thread has 16 columns of a row
+                        const int j = 32 * (quad & 1) + lane, first = 4 * (part & 1) + (quad & 2);
+                        uint32_t hi[8], lo[8];
+                        take_pt<2>(stage + In::PT, stage + In::META, j, first, hi, lo);
+                        uint8_t* const row = sm + L::OFF_PT + j * 128;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int at = ((first + i) ^ (j & 7)) << 4;
+                            *reinterpret_cast<uint4*>(row + at) = make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]);
+                            *reinterpret_cast<uint4*>(row + TILE + at) = make_uint4(lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3]);
+                        }
+                        fence_proxy_async_smem();
+                    }
                     WAIT_HOT(&sh.q_full, cc & 1);
                     tc_fence_after();
 #pragma unroll
@@ -1107,11 +1180,12 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) delta_walk_wide_kernel(const
                         tc_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 16; i += 4) {
-                            const float4 g = *reinterpret_cast<const float4*>(meta + tok + 16 * half + i);
-                            a[i] = __float_as_uint(__uint_as_float(a[i]) * g.x);
-                            a[i + 1] = __float_as_uint(__uint_as_float(a[i + 1]) * g.y);
-                            a[i + 2] = __float_as_uint(__uint_as_float(a[i + 2]) * g.z);
-                            a[i + 3] = __float_as_uint(__uint_as_float(a[i + 3]) * g.w);
+                            const ulonglong2 g = *reinterpret_cast<const ulonglong2*>(meta + DC + tok + 16 * half + i);
+                            const float2 u = unpair(mul2(pair(a[i], a[i + 1]), mul2(g.x, scale))), v = unpair(mul2(pair(a[i + 2], a[i + 3]), mul2(g.y, scale)));
+                            a[i] = __float_as_uint(u.x);
+                            a[i + 1] = __float_as_uint(u.y);
+                            a[i + 2] = __float_as_uint(v.x);
+                            a[i + 3] = __float_as_uint(v.y);
                         }
                         tmem_st16(lane_addr + L::COL_O + tok + 16 * half, a);
                     }
