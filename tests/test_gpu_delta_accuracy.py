@@ -142,3 +142,27 @@ def test_prompt_and_single_tokens_agree(impl, dtype, d):
     differ = (one != all_).double()
     big = one.double().abs() >= 0.1 * one.double().abs().amax((0, 2), keepdim=True)
     assert differ[big].mean() <= 0.27
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_nan_in_a_state_stays_in_its_column(dtype, d):
+    """A slot with a NaN in one column of one head: that column of that row's output and state, and nothing else."""
+    dsla = _dsla()
+    x = _draw(5, 4, 2, d, dtype, 46)
+    slots = torch.tensor([3, 1, -1, 0, 2], dtype=torch.int32, device="cuda")
+    init = _init(4, 4, d, 4, 1.0).cuda()
+    out = []
+    for spoilt in (False, True):
+        st = dsla.dsla_state_alloc_n(4, 1, 4, d, d)
+        st.tensor.copy_(init)
+        if spoilt:
+            st.tensor[1, 0, 2, 7, 37] = float("nan")
+        out.append((dsla.dsla_delta_decode_step(*x, st, slots=slots), st.tensor))
+    (o, s), (o2, s2) = out
+    assert bool(torch.isfinite(o).all()) and bool(torch.isfinite(s).all())
+    bad_o, bad_s = torch.zeros_like(o, dtype=torch.bool), torch.zeros_like(s, dtype=torch.bool)
+    bad_o[1, 2, 37] = True          # row 1 has slot 1
+    bad_s[1, 0, 2, :, 37] = True
+    assert bool(torch.isnan(o2[bad_o]).all()) and bool(torch.isnan(s2[bad_s]).all())
+    assert torch.equal(o[~bad_o], o2[~bad_o]) and torch.equal(s[~bad_s], s2[~bad_s])
