@@ -316,8 +316,9 @@ dsla_status dsla_state_copy(dsla_state* st, const int32_t* src_slots, const int3
  * (I + tril(beta_j D_ji k_j.k_i, -1)) U = beta (V - G K S).
  *   SIMT   : chunks of 16 tokens in fp32 (products of two TF32 terms, 22 bits), every dtype and head size, no workspace.
  *   TENSOR : bf16 (heads of 64 or 128), chunks of 64 tokens on the tensor cores: the inverses of all chunks are computed first, in parallel, into the
- *            workspace, then each (sequence, head) walks its chunks.  Everything that reaches a state is held in 16 bits of mantissa or more and summed
- *            in fp32 (states within 1e-5 of the token-by-token ones).
+ *            workspace, then each (sequence, head) walks its chunks.  Everything that reaches a state or an output is held in 16 bits of mantissa or more and
+ *            summed in fp32: states come out within 3e-5 of the largest value of their head (measured 1.7e-5), outputs within their rounding to bf16
+ *            and 1e-4 of the size of what they are summed from, scale * sum_a |q_a| |S_ab| (measured 3e-6).
  *   AUTO   : TENSOR for bf16, else SIMT.
  * A call that runs TENSOR is refused (DSLA_ERR_INVALID_ARG) without the workspace that dsla_delta_prefill_workspace_bytes() reports.
  * An infinity or NaN in a token reaches, at most, the outputs of its whole chunk and all later ones of its sequence, never those of another sequence.
@@ -369,7 +370,7 @@ dsla_status dsla_delta_decode_step(const dsla_delta_decode_args* a, dsla_state* 
  *     y = w * x * r,   r = 1 / sqrt(mean(x^2) + eps) (RMS),  1 / sqrt(sum(x^2) + eps) (L2),  1 (NONE),
  * and of the first `rot` channels of y each pair (a, b) becomes (a cos f - b sin f, b cos f + a sin f) with the angle
  * f = position * inv_freq[i] (taken in fp64 before it is reduced, so far positions keep their angles): pair i is (i, i + rot/2), or
- * (2i, 2i + 1) where `interleaved` is set.  Arithmetic in fp32, one rounding at the end.  Rows of x are `*_stride` elements apart, heads and channels
+ * (2i, 2i + 1) where `interleaved` is set.  Arithmetic in fp32, the squares too (|x| up to 1e18), one rounding at the end.  Rows of x are `*_stride` elements apart, heads and channels
  * within a row contiguous, so x may be a part of the rows of a fused projection; the outputs have strides of their own and
  * may be the inputs themselves (same pointer and stride; other overlaps are not allowed).  rot a multiple of 16 in 0 .. d, else DSLA_ERR_UNSUPPORTED.
  * Pointers 16-byte aligned and strides multiples of 16 bytes, else DSLA_ERR_INVALID_ARG.  (No counterpart in the paper.)
