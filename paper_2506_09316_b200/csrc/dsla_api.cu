@@ -404,7 +404,6 @@ dsla_status dsla_decode_step(const dsla_decode_args* a, dsla_state* st, void* cu
     return decode_device(a, st, static_cast<cudaStream_t>(cuda_stream));
 }
 
-// ---- gate producer ------------------------------------------------------------------------
 // ---- slots --------------------------------------------------------------------------------
 dsla_status dsla_state_copy(dsla_state* st, const int32_t* src_slots, const int32_t* dst_slots, int n, void* cuda_stream) {
     if (!st || n < 0 || n > 65535 || !on_store_device(st)) return DSLA_ERR_INVALID_ARG;
@@ -496,6 +495,7 @@ dsla_status dsla_qk_norm_rope(const dsla_qk_norm_rope_args* a, void* cuda_stream
     return launch_qk_norm_rope(a, static_cast<cudaStream_t>(cuda_stream));
 }
 
+// ---- gate producer ------------------------------------------------------------------------
 dsla_status dsla_gate_project(const dsla_gate_project_args* a, void* cuda_stream) {
     if (!a || a->T < 0 || a->H <= 0 || a->D_model <= 0) return DSLA_ERR_INVALID_ARG;
     if (a->H % 8 != 0 || 2 * a->H > 256 || a->D_model % 64 != 0) return DSLA_ERR_UNSUPPORTED;
