@@ -4,7 +4,7 @@
 // d_k or a chunk in their middle run as TF32 products of two terms (22 bits, fp32 sums): with plain FMAs each operand is read from shared memory as often as it is used, and the
 // reads took 5600 cycles a chunk.  The state is fp32 in the accumulators' layout, one copy of it in shared memory for K S and Q S.  Products of gates are plain products: a gate of 0 is
 // exact.  Tokens behind a sequence's end have no key, no beta and a gate of 1: they change nothing.
-// Bound by the latency of the preparation, some 3000 cycles a chunk and group: 512 tokens of 4 heads of 64 34 us (one group 68, two 54, four 35; operands stored as
+// Bound by the one SM that the walk and the preparation share: of the 35 us of 512 tokens of 4 heads of 64 the walk takes 23 by itself and the preparation 27 (issue slots 54 % busy; one group 68 us, two 54, four 35; operands stored as
 // their two terms, so that nobody splits them twice, 46: the reads count; token by token, one shuffled sum per token and column, 63 to 112).  It serves fp32, and whoever asks for it; bf16 prompts have dsla_delta_tc.cu.
 #include "dsla_delta.cuh"
 

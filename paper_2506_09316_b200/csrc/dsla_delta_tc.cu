@@ -107,8 +107,8 @@ __device__ __forceinline__ void split_pair(uint64_t x, uint32_t& hi, uint32_t& l
 // into P.  (I + A)^-1 in fp32, in A's place: the eight diagonal blocks of 8 by substitution, one column per thread, then three times
 //     [a 0; b c]^-1 = [a^-1 0; -c^-1 b a^-1 c^-1]
 // for pairs of blocks of 8, 16 and 32, as TF32 products of two terms each (22 bits); a warp takes 16 columns, so that the other factor is split into terms half as often.  Then P T and Y are MMAs, one after the other through
-// the same tiles: 56 KB and 64 registers a thread keep four CTAs on an SM.  4096 tokens of 32 heads: 52 us with 75 KB and three CTAs; 110 us with a substitution over
-// all 64 rows by 64 threads, 2016 steps of the chain each, and T written two bytes at a time.
+// the same tiles: 56 KB and 64 registers a thread keep four CTAs on an SM.  4096 tokens of 32 heads: 54 us (the products of P T's low terms and
+// their packing 3 of them; with 75 KB and three CTAs on an SM 4 % longer; 110 us with a substitution over all 64 rows by 64 threads, 2016 steps of the chain each, and T written two bytes at a time).
 constexpr int PREP_THREADS = 256;
 constexpr int XP = 68;                                          // pitch of A and its inverse in shared memory, floats
 constexpr int PREP_A = 0, PREP_SCRATCH = DC * XP * 4;           // behind K and Q; scratch: [32][8] floats of four pairs of warps
@@ -515,12 +515,12 @@ __global__ void __launch_bounds__(PREP_THREADS, 4) delta_chunk_kernel(const __gr
 //   PT_hi [R_hi | R_lo] + PT_lo R_hi   the same, lanes 64..127, P T out of tensor memory; behind it
 // The state is 16 fp32 registers of each thread (lane = d_k).  Quadrants 0 and 1 make R; 2 and 3 finish the outputs of a chunk while the next one's first product
 // runs, and take its P T apart into tensor memory.  K and Q are free as soon as that product is done, Y and P T with the last: the two groups of a stage have barriers of their own.
-// Bound by shared memory and the chain: a chunk takes 2300 cycles; copies in (78 KB), operands of 24 MMAs (104 KB) and the rows' own accesses hold its port for most of them.
+// Bound by shared memory and the chain: a chunk takes 2360 cycles; copies in (78 KB), operands of 24 MMAs (104 KB) and the rows' own accesses hold its port for most of them.
 // Slices of a sequence, the first kernel for one slice under the walk of the slice before, took as long as one after the other (4096 tokens 151 us).
 // Where the slabs of 32 columns do not all fit on the device at once, fewer and wider ones do more in all: whole heads for d = 128 (delta_walk_wide_kernel), 64 columns for d = 64
-// (32 heads of 64, 64 sequences of 512 tokens: 766 us with W = 32, 578 with W = 64; 80 heads, one sequence of 2048: 145 and 123).  A CTA that is done then takes over a block
+// (32 heads of 64, 64 sequences of 512 tokens: 765 us with W = 32, 571 with W = 64; 80 heads, one sequence of 2048: 135 and 112).  A CTA that is done then takes over a block
 // of the grid that has not started, two of them ahead: the next one's loads run under the end of this one's, and barriers and tensor memory are set up once (64 sequences of 64
-// tokens, 32 heads of 64: 160 us with a CTA for each, 129 so; of 512 tokens 621 and 578).
+// tokens, 32 heads of 64: 181 us with a CTA for each, 127 so; of 512 tokens 631 and 571).
 constexpr int WC = 16, ST = 2;      // columns of a thread; stages of loads
 
 template <int D_, int W_>
@@ -631,7 +631,7 @@ __device__ __forceinline__ bool walk_set_up(WalkShared& sh, const DeltaParams& p
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const bool sorted = p.cu_seqlens && p.N > 1 && p.N <= 128;
-    if (sorted) {      // the longest sequences first (58K tokens in 16 sequences of 1 to 8K: 1.55 ms in the order given, 1.47 so)
+    if (sorted) {      // the longest sequences first (103K tokens in 14 sequences of 1 to 16K, 32 heads of 128: 2.46 ms in the order given, 2.30 so)
         if (tid < p.N) {
             const int mine = p.cu_seqlens[tid + 1] - p.cu_seqlens[tid];
             int rank = 0, from = p.cu_seqlens[0];
@@ -937,8 +937,8 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
 // Sixteen row warps, four to a lane quadrant ("parts"): each has 32 columns of d_k of the state in registers; parts 0 and 1 make R of 32 tokens each, 2 and 3 take P T apart into
 // two tiles, scale Q S and finish the outputs of the chunk before.  V comes transposed through ldmatrix in the fragment layout that R is then stored in, outputs leave through stmatrix.
 // K S is multiplied ahead of Q S, so that R is made under the latter, and the state's columns in two halves, so that half of them are split into terms under the other half's product.
-// Bound by the chain, 3750 cycles a chunk, with HBM at 5 TB/s and the tensor pipe 54 % busy behind it (58K ragged tokens, 32 heads, both kernels: 1.90 ms in slabs of 32 columns, 1.59 in slabs of
-// 64, 1.29 so; 40 heads, one sequence of 2048 tokens, 40 CTAs instead of 160: 133 us in slabs of 32, 113 so).
+// Bound by the chain, 3750 cycles a chunk, with HBM at 5 TB/s and the tensor pipe 54 % busy behind it (103K ragged tokens, 32 heads, both kernels: 3.15 ms in slabs of 32 columns, 2.30 so; slabs
+// of 64 lay half-way; 40 heads, one sequence of 2048 tokens, 40 CTAs instead of 160: 120 us in slabs of 32, 105 so).
 struct Wide {
     using In = Chunk<128>;
     static constexpr int D = 128, W = 128, ROW_WARPS = 16, THREADS = 32 * (ROW_WARPS + 2);
