@@ -937,7 +937,7 @@ __global__ void __launch_bounds__(Walk<D, W>::THREADS, 1) delta_walk_kernel(cons
 // Sixteen row warps, four to a lane quadrant ("parts"): each has 32 columns of d_k of the state in registers; parts 0 and 1 make R of 32 tokens each, 2 and 3 take P T apart into
 // two tiles, scale Q S and finish the outputs of the chunk before.  V comes transposed through ldmatrix in the fragment layout that R is then stored in, outputs leave through stmatrix.
 // K S is multiplied ahead of Q S, so that R is made under the latter, and the state's columns in two halves, so that half of them are split into terms under the other half's product.
-// Bound by the chain, 3750 cycles a chunk, with HBM at 5 TB/s and the tensor pipe 54 % busy behind it (103K ragged tokens, 32 heads, both kernels: 3.15 ms in slabs of 32 columns, 2.30 so; slabs
+// Bound by the chain, 4400 cycles a chunk with all that is around it, HBM at 5 TB/s and the tensor pipe 57 % busy (103K ragged tokens, 32 heads, both kernels: 3.15 ms in slabs of 32 columns, 2.30 so; slabs
 // of 64 lay half-way; 40 heads, one sequence of 2048 tokens, 40 CTAs instead of 160: 120 us in slabs of 32, 105 so).
 struct Wide {
     using In = Chunk<128>;
